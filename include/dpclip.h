@@ -503,6 +503,87 @@ int dpclip_read_status(const void* workspace, int* host_status /* host */, void*
 /* Which form DPCLIP_AUTO resolves to for this layer (a dpclip_method). */
 int dpclip_pick_method(int B, int T, int d_in, int d_out, long lda, long ldz, dpclip_dtype dtype);
 
+/* ---------------------------------------------------------------------------
+ * Operators of a transformer block.  The method needs of a layer its input and the signal at its output; the entry points below are the
+ * passes around the layers above whose parameters or signals a step could not take: the learned relative position bias, the norms of
+ * queries and keys with the rotation, and the gated feed-forward block (further down).  Where they have parameters of a few hundred
+ * numbers, their norm call leaves the per-example gradients G_i in memory the caller owns ("The sum over the positions that share a
+ * parameter is taken before the norm", Sec. "LayerNorm Layers") and one more row of sq_layers [L][B] for dpclip_factors; the clipped sum
+ * is then dpclip_stored_clipped_grad.  Sums are fp32 in a fixed order: the same call gives the same bits.  A sum that leaves fp32
+ * is an infinity and propagates like an infinite input.
+ * ------------------------------------------------------------------------- */
+
+/* Clipped sum of stored per-example gradients: g[j] = sum_i clip[i] grads[i][j] + sigma C xi_j, j in [0, n).
+ *   grads  [B][ld] fp32, ld >= n;  clip [B] or NULL (all ones);  g [n] fp32, OVERWRITTEN
+ *   noise  as dpclip_add_noise on g for (seed, stream_id); sigma * C == 0 adds none
+ * Errors: INVALID_ARG (null pointer, B or n <= 0, ld < n, negative sigma or C), MISALIGNED. */
+int dpclip_stored_clipped_grad(const float* grads, long ld, int B, int n, const float* clip, float* g, float sigma, float C,
+                               unsigned long long seed, unsigned long long stream_id, void* stream);
+
+/* Learned relative position bias by buckets (attention scores S[h][q][k] += table[bucket][h]).  Query q is at position q_offset + q, key k
+ * at position k; the bucket goes by the distance k - (q_offset + q):
+ *   bidirectional != 0: half of the buckets for keys at or before the query, half for keys behind it; n = n_buckets / 2, d = |distance|
+ *   bidirectional == 0: keys behind the query count as distance zero; n = n_buckets, d = max(-distance, 0)
+ *   d < e = n / 2: bucket d;  else e + floor((n - e) log(d / e) / log(max_distance / e)), at most n - 1 (whole numbers of the logarithm
+ *   count as such)
+ * causal != 0: keys behind the query are masked: -inf in the forward pass, not read by the gradient.
+ * n_buckets 2..256 (bidirectional: even and at least 4), max_distance in (e, 2^24]. */
+typedef struct { int n_buckets, max_distance, bidirectional, causal; } dpclip_relbias;
+/* The bucket of a distance (host function, no launch), or INVALID_ARG. */
+int dpclip_relbias_bucket(const dpclip_relbias* config /* host */, long distance);
+/* bias[h][q][k], h < H, q < Tq, k < Tk.
+ *   table  [n_buckets][ldt] fp32, ldt >= H;  bias: `dtype`, row stride ld >= Tk, head stride head_stride (elements), OVERWRITTEN
+ *          where k < Tk (what lies between the rows stays)
+ * Tq = 1 with q_offset is the row of one decoded token.  Errors: INVALID_ARG, MISALIGNED. */
+int dpclip_relbias_forward(const float* table, long ldt, const dpclip_relbias* config /* host */, int H, int Tq, int Tk, long q_offset,
+                           dpclip_dtype dtype, void* bias, long ld, long head_stride, void* stream);
+/* Per-example gradients of the table, G_i[b][h] = sum of dS_i[h][q][k] over the pairs (q, k) of bucket b, and their squared norms.
+ *   dS        signal at the scores, element (i, h, q, k) at i * example_stride + h * head_stride + q * ld + k, `dtype`
+ *   q_lens, k_lens  [B] device or NULL: example i has queries q < q_lens[i] and keys k < k_lens[i]; lengths outside [0, Tq] / [0, Tk]
+ *             count as the nearest.  Pairs outside the lengths or the causal mask do not count, whatever dS holds there.
+ *   accumulate  0: grads is overwritten; 1: added to (one table used by several layers: call per layer, the norm is then that
+ *             of the sum over the layers so far, which is what the whole gradient needs)
+ *   grads     [B][n_buckets][H] fp32;  sq_layer [B] fp32, OVERWRITTEN with ||G_i||^2
+ *   workspace >= dpclip_relbias_workspace_bytes()
+ * Errors: INVALID_ARG, MISALIGNED, WORKSPACE, UNSUPPORTED (more than 2^31 tiles). */
+int dpclip_relbias_sqnorms(const void* dS, long ld, long head_stride, long example_stride, int B, int H, int Tq, int Tk, long q_offset,
+                           const int* q_lens, const int* k_lens, const dpclip_relbias* config /* host */, dpclip_dtype dtype,
+                           int accumulate, float* grads, float* sq_layer, void* workspace, size_t workspace_bytes, void* stream);
+size_t dpclip_relbias_workspace_bytes(int B, int H, int Tq, int Tk, int n_buckets, dpclip_dtype dtype);
+
+/* Norms of queries and keys with the rotation in the same pass.  Each head x of D elements:
+ *   y = R_pos (gain (.) x / sqrt(mean(x^2) + eps))
+ * R_pos turns the pairs of the first rot_dim elements by the angles of the token's position: pair i is (i, rot_dim / 2 + i), or
+ * (2 i, 2 i + 1) when `interleaved`; the other elements stay.
+ *   parts     n_parts (1 or 2) tensors that share positions and widths, queries and keys: element (i, t, h, d) at
+ *             i * example + t * token + h * head + d elements of its pointer, so rows of a joint projection and head-major tensors are
+ *             read in place.  gain [D] fp32 or NULL (ones; no gradient).  `out` may be `x` itself (same strides).
+ *   table     [n_pos][2][rot_dim / 2] fp32, cosines then sines (dpclip_rotation_table, or any other angles); NULL when rot_dim == 0
+ *   positions [B * T] device or NULL: position pos0 + t.  A token whose position is negative or not below n_pos is padding: the forward
+ *             pass leaves its rows of `out` as they are, the backward pass writes zeros there and counts nothing of it.
+ * D <= 512, any width and alignment; widths and strides in multiples of 16 bytes are fastest.
+ * Errors: INVALID_ARG, MISALIGNED, UNSUPPORTED (D > 512, B * T above 2^31 - 4097; backward: B > 65535, T * H above 2^30). */
+typedef struct {
+    const void* x;  long x_example, x_token, x_head;
+    const void* dy; long dy_example, dy_token, dy_head;     /* backward: signal at the output; else NULL */
+    void* out;      long out_example, out_token, out_head;  /* forward: y; backward: dx (may be dy itself) */
+    int H;
+    const float* gain;
+} dpclip_heads;
+int dpclip_qknorm_forward(const dpclip_heads* parts /* host */, int n_parts, int B, int T, int D, int rot_dim, int interleaved,
+                          const float* table, long n_pos, const int* positions, long pos0, float eps, dpclip_dtype dtype, void* stream);
+/* From dy: dx, and per example the gain's gradient G_i[d] = sum over t and h of (R_pos^T dy)_d x_d / sqrt(mean(x^2) + eps).
+ *   grads      host array of n_parts device pointers, [B][D] fp32 each, OVERWRITTEN, or NULL entries
+ *   sq_layers  host array of n_parts device pointers, [B] fp32 each, OVERWRITTEN with ||G_i||^2 (a row of sq_layers [L][B]), or NULL entries
+ *   workspace >= dpclip_qknorm_workspace_bytes(), WORKSPACE otherwise */
+int dpclip_qknorm_backward(const dpclip_heads* parts /* host */, int n_parts, int B, int T, int D, int rot_dim, int interleaved,
+                           const float* table, long n_pos, const int* positions, long pos0, float eps, dpclip_dtype dtype,
+                           float* const* grads /* host */, float* const* sq_layers /* host */, void* workspace, size_t workspace_bytes,
+                           void* stream);
+size_t dpclip_qknorm_workspace_bytes(int B, int T, int Hq, int Hk, int D);
+/* Angles of n_pos positions: pos * base^(-2 i / rot_dim) / scale, computed in 64 bits. */
+int dpclip_rotation_table(float* table, long n_pos, int rot_dim, double base, double scale, void* stream);
+
 /* Number of kernels this library has launched in this process (a host-side
  * counter for benchmarks and tests; cudaMemset calls are not counted, nor is the
  * kernel that stands for them in a step on several streams). */

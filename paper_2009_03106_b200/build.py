@@ -13,7 +13,7 @@ LIB = os.path.join(HERE, "libdpclip.so")
 LIB_DEBUG = os.path.join(HERE, "libdpclip_debug.so")       # -DDPCLIP_DEBUG: range-checked accesses
 
 NVCC_FLAGS = ["-std=c++17", "-O3", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo",
-              "-Xcompiler", "-fPIC", "-shared", "-I" + INCLUDE, "-I" + CSRC]
+              "-Xcompiler", "-fPIC", "-I" + INCLUDE, "-I" + CSRC]
 
 
 def sources():
@@ -28,17 +28,42 @@ def _stale(lib: str = LIB) -> bool:
     return any(os.path.getmtime(d) > t for d in deps)
 
 
+def _object_stale(obj: str, dep: str) -> bool:
+    """Whether an object file is older than its source or any header it was compiled from (nvcc -MD writes the list)."""
+    if not (os.path.exists(obj) and os.path.exists(dep)):
+        return True
+    with open(dep) as f:
+        names = f.read().replace("\\\n", " ").split(":", 1)[1].split()
+    t = os.path.getmtime(obj)
+    own = [n for n in names if os.path.abspath(n).startswith(os.path.dirname(HERE))]
+    return any(not os.path.exists(n) or os.path.getmtime(n) > t for n in own)
+
+
 def build(force: bool = False, verbose: bool = False, debug: bool = False) -> str:
-    """Compile every .cu under csrc/ into one shared library.  Returns its path.
+    """Compile every .cu under csrc/, each to an object of its own and all at once, and link one shared library.  Returns its path.
     debug=True builds libdpclip_debug.so (range-checked accesses that set DPCLIP_ERR_RANGE and skip) beside it."""
     lib = LIB_DEBUG if debug else LIB
     if not force and not _stale(lib):
         return lib
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
+    objects = os.path.join(HERE, "build", "debug" if debug else "release")
+    os.makedirs(objects, exist_ok=True)
+    flags = NVCC_FLAGS + (["-DDPCLIP_DEBUG"] if debug else []) + (["-Xptxas", "-v"] if verbose else [])
+    running, objs = [], []
+    for src in sources():
+        name = os.path.splitext(os.path.basename(src))[0]
+        obj, dep = os.path.join(objects, name + ".o"), os.path.join(objects, name + ".d")
+        objs.append(obj)
+        if force or verbose or _object_stale(obj, dep):
+            tmp = f"{obj}.tmp{os.getpid()}.o"
+            cmd = [nvcc] + flags + ["-c", src, "-o", tmp, "-MD", "-MF", dep]
+            running.append((cmd, tmp, obj, subprocess.Popen(cmd)))
+    for cmd, tmp, obj, p in running:
+        if p.wait() != 0:
+            raise subprocess.CalledProcessError(p.returncode, cmd)
+        os.replace(tmp, obj)
     tmp = lib + f".tmp{os.getpid()}"
-    cmd = ([nvcc] + NVCC_FLAGS + (["-DDPCLIP_DEBUG"] if debug else []) + (["-Xptxas", "-v"] if verbose else []) +
-           sources() + ["-o", tmp])
-    subprocess.check_call(cmd)
+    subprocess.check_call([nvcc] + NVCC_FLAGS + ["-shared"] + objs + ["-o", tmp])
     os.replace(tmp, lib)
     return lib
 

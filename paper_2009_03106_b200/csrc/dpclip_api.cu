@@ -3,6 +3,7 @@
 #include <string.h>
 
 #include "common.cuh"
+#include "internal.cuh"
 #include <math.h>
 
 #include "kernels_simt.cuh"
@@ -1678,6 +1679,17 @@ int try_fused_t1_step(const dpclip_layer* layers, int L, int B, dpclip_dtype dty
 }
 
 }  // namespace
+
+// what the other translation units use of this one (internal.cuh)
+namespace dpclip {
+int finish_launch() { return launch_status(); }
+bool overlap_allowed() { return !path_switch(SW_NO_OVERLAP); }
+bool tensor_cores_allowed() { return !path_switch(SW_FORCE_SIMT); }
+void log_line(const char* text) { DPCLIP_LOGF("%s", text); }
+bool encode_map_bf16(CUtensorMap* map, const void* base, long rows, long cols, long ld, int box_cols, int box_rows) {
+    return make_map_bf16(map, base, rows, cols, ld, box_cols, box_rows);
+}
+}  // namespace dpclip
 
 extern "C" {
 

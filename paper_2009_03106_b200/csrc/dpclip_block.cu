@@ -1,0 +1,338 @@
+// C ABI of the operators of a transformer block: argument checks, how the work is cut, launches.
+#include <math.h>
+#include <stdint.h>
+#include <string.h>
+
+#include "internal.cuh"
+#include "kernels_qknorm.cuh"
+#include "kernels_relbias.cuh"
+#include "kernels_stored.cuh"
+
+using namespace dpclip;
+
+namespace {
+
+inline size_t elt_size(dpclip_dtype dt) { return dt == DPCLIP_F32 ? 4 : 2; }
+inline bool dtype_known(dpclip_dtype dt) { return dt == DPCLIP_F32 || dt == DPCLIP_BF16; }
+inline size_t round_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
+inline int clamp_int(long v, long lo, long hi) { return (int)(v < lo ? lo : v > hi ? hi : v); }
+
+// ------------------------------------------------------------------------------------------------ relative position bias
+// thr[k], the smallest distance d of bucket exact + k: floor((n - exact) log(d / exact) / log(max / exact)) >= k, which is
+// d >= exact (max / exact)^(k / (n - exact)).  Borders that are whole numbers belong to the upper bucket; the powers are taken in extended
+// precision, where a border that is a whole number misses it by less than 1e-15 of itself.
+bool fill_buckets(RbBuckets& r, const dpclip_relbias* c) {
+    if (!c || c->n_buckets < 2 || c->n_buckets > RB_MAX_BUCKETS) return false;
+    if (c->bidirectional && c->n_buckets % 2) return false;
+    memset(&r, 0, sizeof(r));
+    r.n_buckets = c->n_buckets;
+    r.n = c->bidirectional ? c->n_buckets / 2 : c->n_buckets;
+    r.exact = r.n / 2;
+    r.max_distance = c->max_distance;
+    r.bidirectional = c->bidirectional != 0;
+    r.causal = c->causal != 0;
+    if (r.exact < 1 || r.max_distance <= r.exact || r.max_distance > (1 << 24)) return false;
+    const int m = r.n - r.exact;
+    const long double ratio = (long double)r.max_distance / r.exact;
+    for (int k = 0; k < m; ++k) {
+        const long double border = r.exact * powl(ratio, (long double)k / m), whole = roundl(border);
+        r.thr[k] = (int)(fabsl(border - whole) < 1e-12L * border ? whole : ceill(border));
+    }
+    return true;
+}
+
+// A tile of the gradient: G groups of nr block rows by KT block columns, 256 threads.
+struct RbTiles { int E, nqb, nkb, KT, G, nr, qtiles, ktiles; };
+RbTiles relbias_tiles(int B, int H, int Tq, int Tk, bool blocks8) {
+    RbTiles t;
+    t.E = blocks8 ? 8 : 1;
+    t.nqb = ceil_div(Tq, t.E); t.nkb = ceil_div(Tk, t.E);
+    const int most = blocks8 ? RB_THREADS : 4 * RB_THREADS;       // four walks a thread where a walk has one sum
+    t.KT = t.nkb < most ? t.nkb : most;
+    t.ktiles = ceil_div(t.nkb, t.KT);
+    t.G = RB_THREADS / t.KT;
+    if (t.G < 1) t.G = 1;
+    if (t.G > t.nqb) t.G = t.nqb;
+    // long walks, as long as there are six CTAs an SM and 40 KB of shared memory hold the sums
+    const int longest = blocks8 ? 32 : 128;
+    t.nr = 1;
+    auto fits = [&](int nr) { return (blocks8 ? rb_smem_floats<8>(t.KT, t.G, nr) : rb_smem_floats<1>(t.KT, t.G, nr)) * sizeof(float) <= 40 * 1024; };
+    while (t.nr < longest && t.G * t.nr < t.nqb && fits(2 * t.nr) &&
+           (long)B * H * t.ktiles * ceil_div(t.nqb, (long)t.G * t.nr * 2) >= 6L * kNumSMs) t.nr *= 2;
+    // rows of single elements are walked eight at a time at least: fewer would be all set-up
+    if (!blocks8) while (t.nr < 8 && t.G * t.nr < t.nqb) t.nr *= 2;
+    t.qtiles = ceil_div(t.nqb, (long)t.G * t.nr);
+    return t;
+}
+inline size_t relbias_part_bytes(const RbTiles& t, int B, int H, int n_buckets) {
+    return sizeof(float) * (size_t)B * H * t.qtiles * t.ktiles * n_buckets;
+}
+
+template <typename T, int E>
+int launch_relbias_forward(RbForward& p, cudaStream_t st) {
+    p.nqb = ceil_div(p.Tq, E); p.nkb = ceil_div(p.Tk, E);
+    // a walk of several block rows pays for its look-ups; at least 64 warps of walks an SM
+    const long blocks = (long)p.nqb * p.nkb * p.H;
+    p.nr = clamp_int(blocks / (kNumSMs * 64L * 32), 1, E == 1 ? 64 : 32);
+    if (p.nr > p.nqb) p.nr = p.nqb;
+    p.chunks = ceil_div(p.nqb, p.nr);
+    p.items = (long)p.H * p.chunks * p.nkb;
+    const long grid = (p.items + RB_THREADS - 1) / RB_THREADS;
+    if (grid > 0x7FFFFFFFL) return DPCLIP_ERR_UNSUPPORTED;
+    relbias_forward_kernel<T, E><<<(unsigned)grid, RB_THREADS, 0, st>>>(p);
+    return finish_launch();
+}
+
+template <typename T, int E>
+int launch_relbias_grad(const RbGrad& p, cudaStream_t st) {
+    const int smem = rb_smem_floats<E>(p.KT, p.G, p.nr) * (int)sizeof(float);
+    relbias_grad_kernel<T, E><<<(unsigned)((long)p.B * p.H * p.qtiles * p.ktiles), RB_THREADS, smem, st>>>(p);
+    return finish_launch();
+}
+
+// ------------------------------------------------------------------------------------------------ norms of queries and keys
+struct QkShape { int V, NCH, G; };        // elements a run, chunks a lane, lanes a head
+bool qk_shape(QkShape& s, int D, int rot, bool vec, dpclip_dtype dtype) {
+    const int v = dtype == DPCLIP_F32 ? 4 : 8;
+    if (vec && D % (2 * v) == 0 && rot % (2 * v) == 0 && D / (2 * v) <= 32) {
+        s.V = v; s.NCH = 1; s.G = 1;
+        while (s.G < D / (2 * v)) s.G *= 2;
+        return true;
+    }
+    s.V = 1; s.G = 32;
+    const int pairs = (D + 1) / 2;
+    s.NCH = pairs <= 32 ? 1 : pairs <= 64 ? 2 : pairs <= 128 ? 4 : 8;
+    return pairs <= 256;
+}
+
+template <typename T, int V, int NCH, int G>
+int launch_qk_forward(QkParams& p, cudaStream_t st) {
+    for (int k = 0; k < 2; ++k) p.part[k].blocks = ceil_div(p.part[k].H, 32 / G);
+    const long blocks = p.part[0].blocks + p.part[1].blocks, tokens = (long)p.B * p.T;
+    if (blocks > 65535) return DPCLIP_ERR_UNSUPPORTED;
+    // four heads in flight a group where that leaves eight warps an SM, else one: short calls are a chain of round trips
+    constexpr int U = NCH == 1 ? 4 : 2;
+    const bool many = tokens * blocks / U >= 8L * kNumSMs;
+    const long warps = (tokens + (many ? U : 1) - 1) / (many ? U : 1);
+    const dim3 grid((unsigned)((warps * 32 + QK_THREADS - 1) / QK_THREADS), (unsigned)blocks);
+    if (many) qknorm_forward_kernel<T, V, NCH, G, U><<<grid, QK_THREADS, 0, st>>>(p);
+    else qknorm_forward_kernel<T, V, NCH, G, 1><<<grid, QK_THREADS, 0, st>>>(p);
+    return finish_launch();
+}
+template <typename T, int V, int NCH, int G>
+int launch_qk_backward(const QkParams& p, cudaStream_t st) {
+    constexpr int U = NCH <= 2 ? 2 : 1;
+    const dim3 grid(p.part[0].chunks + p.part[1].chunks, p.B);
+    const size_t smem = sizeof(float) * (QK_THREADS / 32) * p.D;
+    qknorm_backward_kernel<T, V, NCH, G, U><<<grid, QK_THREADS, smem, st>>>(p);
+    return finish_launch();
+}
+template <typename T>
+int launch_qk(QkParams& p, const QkShape& s, bool backward, cudaStream_t st) {
+    constexpr int VV = sizeof(T) == 4 ? 4 : 8;
+#define DPCLIP_QK(V, NCH, G) return backward ? launch_qk_backward<T, V, NCH, G>(p, st) : launch_qk_forward<T, V, NCH, G>(p, st)
+    if (s.V == 1) switch (s.NCH) { case 1: DPCLIP_QK(1, 1, 32); case 2: DPCLIP_QK(1, 2, 32); case 4: DPCLIP_QK(1, 4, 32); default: DPCLIP_QK(1, 8, 32); }
+    switch (s.G) {
+        case 1: DPCLIP_QK(VV, 1, 1); case 2: DPCLIP_QK(VV, 1, 2); case 4: DPCLIP_QK(VV, 1, 4);
+        case 8: DPCLIP_QK(VV, 1, 8); case 16: DPCLIP_QK(VV, 1, 16); default: DPCLIP_QK(VV, 1, 32);
+    }
+#undef DPCLIP_QK
+}
+
+// CTAs an example for `items` warp items of one part: about four CTAs an SM in all, at least sixteen items a CTA
+inline int qk_chunks(int B, long items) { return clamp_int(ceil_div(4L * kNumSMs, B), 1, items / 16 > 0 ? items / 16 : 1); }
+// most chunks any form of the kernels makes, for the workspace: one head a warp item
+inline int qk_most_chunks(int B, int T, int H) { return H > 0 ? qk_chunks(B, (long)T * H) : 0; }
+
+int qk_check(const dpclip_heads* parts, int n_parts, int B, int T, int D, int rot_dim, const float* table, long n_pos,
+             const int* positions, long pos0, float eps, dpclip_dtype dtype, bool backward) {
+    if (!parts || n_parts < 1 || n_parts > 2 || B <= 0 || T <= 0 || D <= 0 || !dtype_known(dtype)) return DPCLIP_ERR_INVALID_ARG;
+    if (rot_dim < 0 || rot_dim > D || rot_dim % 2 || !(eps >= 0.f) || n_pos <= 0) return DPCLIP_ERR_INVALID_ARG;
+    if ((rot_dim > 0 && !table) || (!positions && pos0 < 0)) return DPCLIP_ERR_INVALID_ARG;
+    if ((long)B * T > 0x7FFFFFFFL - 4096 || D > 512 || (backward && B > 65535)) return DPCLIP_ERR_UNSUPPORTED;
+    const size_t es = elt_size(dtype);
+    for (int k = 0; k < n_parts; ++k) {
+        const dpclip_heads& h = parts[k];
+        if (!h.x || !h.out || (backward && !h.dy) || h.H <= 0) return DPCLIP_ERR_INVALID_ARG;
+        if (!is_aligned(h.x, es) || !is_aligned(h.out, es) || (h.dy && !is_aligned(h.dy, es)) || (h.gain && !is_aligned(h.gain, 4)))
+            return DPCLIP_ERR_MISALIGNED;
+    }
+    if ((table && !is_aligned(table, 4)) || (positions && !is_aligned(positions, 4))) return DPCLIP_ERR_MISALIGNED;
+    return DPCLIP_OK;
+}
+
+// fills p; whether every run of V elements is a 16-byte load
+bool qk_fill(QkParams& p, const dpclip_heads* parts, int n_parts, int B, int T, int D, int rot_dim, int interleaved, const float* table,
+             long n_pos, const int* positions, long pos0, float eps, dpclip_dtype dtype, bool backward) {
+    memset(&p, 0, sizeof(p));
+    p.B = B; p.T = T; p.D = D; p.rot = rot_dim; p.interleaved = interleaved != 0;
+    p.n_pos = n_pos; p.pos0 = pos0; p.pos = positions; p.table = table; p.eps = eps;
+    const long v = dtype == DPCLIP_F32 ? 4 : 8;
+    bool vec = !table || is_aligned(table, 16);
+    for (int k = 0; k < n_parts; ++k) {
+        const dpclip_heads& h = parts[k];
+        QkPart& q = p.part[k];
+        q.x = h.x; q.xb = h.x_example; q.xt = h.x_token; q.xh = h.x_head;
+        q.y = h.out; q.ob = h.out_example; q.ot = h.out_token; q.oh = h.out_head;
+        q.dy = h.dy; q.yb = h.dy_example; q.yt = h.dy_token; q.yh = h.dy_head;
+        q.gain = h.gain; q.H = h.H;
+        // an extent of one: its stride is never used
+        if (B == 1) q.xb = q.ob = q.yb = 0;
+        if (T == 1) q.xt = q.ot = q.yt = 0;
+        if (h.H == 1) q.xh = q.oh = q.yh = 0;
+        vec = vec && is_aligned(h.x, 16) && is_aligned(h.out, 16) && (!h.gain || is_aligned(h.gain, 16));
+        vec = vec && (q.xb | q.xt | q.xh | q.ob | q.ot | q.oh) % v == 0;
+        if (backward) vec = vec && is_aligned(h.dy, 16) && (q.yb | q.yt | q.yh) % v == 0;
+    }
+    return vec;
+}
+
+}  // namespace
+
+extern "C" {
+
+int dpclip_stored_clipped_grad(const float* grads, long ld, int B, int n, const float* clip, float* g, float sigma, float C,
+                               unsigned long long seed, unsigned long long stream_id, void* stream) {
+    if (!grads || !g || B <= 0 || n <= 0 || ld < n || !(sigma >= 0.f) || !(C >= 0.f)) return DPCLIP_ERR_INVALID_ARG;
+    if (!is_aligned(grads, 4) || !is_aligned(g, 4) || (clip && !is_aligned(clip, 4))) return DPCLIP_ERR_MISALIGNED;
+    StoredParams p;
+    memset(&p, 0, sizeof(p));
+    p.G = grads; p.ld = ld; p.B = B; p.n = n; p.clip = clip; p.g = g; p.noise_scale = sigma * C;
+    p.k0 = (uint32_t)seed; p.k1 = (uint32_t)(seed >> 32); p.s0 = (uint32_t)stream_id; p.s1 = (uint32_t)(stream_id >> 32);
+    cudaStream_t st = (cudaStream_t)stream;
+    if (B > 256) stored_grad_kernel<32><<<ceil_div(n, 32), 1024, 0, st>>>(p);
+    else stored_grad_kernel<8><<<ceil_div(n, 32), 256, 0, st>>>(p);
+    return finish_launch();
+}
+
+int dpclip_relbias_bucket(const dpclip_relbias* config, long distance) {
+    RbBuckets r;
+    if (!fill_buckets(r, config)) return DPCLIP_ERR_INVALID_ARG;
+    return rb_bucket(r, distance);
+}
+
+int dpclip_relbias_forward(const float* table, long ldt, const dpclip_relbias* config, int H, int Tq, int Tk, long q_offset,
+                           dpclip_dtype dtype, void* bias, long ld, long head_stride, void* stream) {
+    RbForward p;
+    memset(&p, 0, sizeof(p));
+    if (!table || !bias || H <= 0 || Tq <= 0 || Tk <= 0 || q_offset < 0 || !dtype_known(dtype)) return DPCLIP_ERR_INVALID_ARG;
+    if (!fill_buckets(p.r, config) || ldt < H || ld < Tk) return DPCLIP_ERR_INVALID_ARG;
+    // rows of different heads must not overlap: heads one behind the other, or side by side in every row
+    if (H > 1 && head_stride < (long)(Tq - 1) * ld + Tk && (head_stride < Tk || ld < (long)(H - 1) * head_stride + Tk))
+        return DPCLIP_ERR_INVALID_ARG;
+    if (!is_aligned(table, 4) || !is_aligned(bias, elt_size(dtype))) return DPCLIP_ERR_MISALIGNED;
+    p.table = table; p.ldt = ldt; p.out = bias; p.ld = ld; p.hs = H > 1 ? head_stride : 0;
+    p.H = H; p.Tq = Tq; p.Tk = Tk; p.off = q_offset;
+    const long v = dtype == DPCLIP_F32 ? 4 : 8;
+    const bool vec = is_aligned(bias, 16) && (Tq == 1 || ld % v == 0) && p.hs % v == 0;
+    cudaStream_t st = (cudaStream_t)stream;
+    if (dtype == DPCLIP_F32) return vec ? launch_relbias_forward<float, 8>(p, st) : launch_relbias_forward<float, 1>(p, st);
+    return vec ? launch_relbias_forward<__nv_bfloat16, 8>(p, st) : launch_relbias_forward<__nv_bfloat16, 1>(p, st);
+}
+
+size_t dpclip_relbias_workspace_bytes(int B, int H, int Tq, int Tk, int n_buckets, dpclip_dtype dtype) {
+    if (!dtype_known(dtype) || B <= 0 || H <= 0 || Tq <= 0 || Tk <= 0 || n_buckets <= 0) return kHeaderBytes;
+    const size_t a = relbias_part_bytes(relbias_tiles(B, H, Tq, Tk, true), B, H, n_buckets);
+    const size_t b = relbias_part_bytes(relbias_tiles(B, H, Tq, Tk, false), B, H, n_buckets);
+    return kHeaderBytes + round_up(a > b ? a : b, 256);
+}
+
+int dpclip_relbias_sqnorms(const void* dS, long ld, long head_stride, long example_stride, int B, int H, int Tq, int Tk, long q_offset,
+                           const int* q_lens, const int* k_lens, const dpclip_relbias* config, dpclip_dtype dtype, int accumulate,
+                           float* grads, float* sq_layer, void* workspace, size_t workspace_bytes, void* stream) {
+    RbGrad p;
+    memset(&p, 0, sizeof(p));
+    if (!dS || !grads || !sq_layer || B <= 0 || H <= 0 || Tq <= 0 || Tk <= 0 || q_offset < 0 || !dtype_known(dtype))
+        return DPCLIP_ERR_INVALID_ARG;
+    if (!fill_buckets(p.r, config) || (Tq > 1 && ld < Tk)) return DPCLIP_ERR_INVALID_ARG;
+    if (H > 1 && head_stride < 0) return DPCLIP_ERR_INVALID_ARG;
+    if (B > 1 && example_stride < 0) return DPCLIP_ERR_INVALID_ARG;
+    const size_t es = elt_size(dtype);
+    if (!is_aligned(dS, es) || !is_aligned(grads, 4) || !is_aligned(sq_layer, 4) || (q_lens && !is_aligned(q_lens, 4)) ||
+        (k_lens && !is_aligned(k_lens, 4))) return DPCLIP_ERR_MISALIGNED;
+    p.dS = dS; p.ld = Tq > 1 ? ld : Tk; p.hs = H > 1 ? head_stride : 0; p.bs = B > 1 ? example_stride : 0;
+    const long v = dtype == DPCLIP_F32 ? 4 : 8;
+    const bool vec = is_aligned(dS, 16) && (Tq == 1 || ld % v == 0) && p.hs % v == 0 && p.bs % v == 0;
+    const RbTiles t = relbias_tiles(B, H, Tq, Tk, vec);
+    const size_t need = kHeaderBytes + relbias_part_bytes(t, B, H, p.r.n_buckets);
+    if (!workspace || workspace_bytes < need || !is_aligned(workspace, 16)) return DPCLIP_ERR_WORKSPACE;
+    const long tiles = (long)t.qtiles * t.ktiles;
+    if ((long)B * H > 0x7FFFFFFFL / tiles) return DPCLIP_ERR_UNSUPPORTED;
+    p.B = B; p.H = H; p.Tq = Tq; p.Tk = Tk; p.nqb = t.nqb; p.nkb = t.nkb; p.KT = t.KT; p.G = t.G; p.nr = t.nr;
+    p.qtiles = t.qtiles; p.ktiles = t.ktiles; p.off = q_offset; p.q_lens = q_lens; p.k_lens = k_lens;
+    p.part = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + kHeaderBytes);
+    cudaStream_t st = (cudaStream_t)stream;
+    int rc;
+    if (dtype == DPCLIP_F32) rc = vec ? launch_relbias_grad<float, 8>(p, st) : launch_relbias_grad<float, 1>(p, st);
+    else rc = vec ? launch_relbias_grad<__nv_bfloat16, 8>(p, st) : launch_relbias_grad<__nv_bfloat16, 1>(p, st);
+    if (rc) return rc;
+    int lanes = 1;
+    while (lanes < 32 && lanes < tiles) lanes *= 2;
+    return launch_after(relbias_finish_kernel, dim3(B), RB_FINISH_THREADS, 0, st, (const float*)p.part, H, (int)tiles, p.r.n_buckets,
+                        lanes, accumulate ? 1 : 0, grads, sq_layer);
+}
+
+int dpclip_rotation_table(float* table, long n_pos, int rot_dim, double base, double scale, void* stream) {
+    if (!table || n_pos <= 0 || rot_dim <= 0 || rot_dim % 2 || !(base > 0.0) || !(scale > 0.0)) return DPCLIP_ERR_INVALID_ARG;
+    if (!is_aligned(table, 4)) return DPCLIP_ERR_MISALIGNED;
+    const long n = n_pos * (rot_dim / 2);
+    const long blocks = (n + 255) / 256;
+    rotation_table_kernel<<<clamp_int(blocks, 1, kNumSMs * 16), 256, 0, (cudaStream_t)stream>>>(table, n_pos, rot_dim, log(base), 1.0 / scale);
+    return finish_launch();
+}
+
+int dpclip_qknorm_forward(const dpclip_heads* parts, int n_parts, int B, int T, int D, int rot_dim, int interleaved,
+                          const float* table, long n_pos, const int* positions, long pos0, float eps, dpclip_dtype dtype, void* stream) {
+    int rc = qk_check(parts, n_parts, B, T, D, rot_dim, table, n_pos, positions, pos0, eps, dtype, false);
+    if (rc) return rc;
+    QkParams p;
+    const bool vec = qk_fill(p, parts, n_parts, B, T, D, rot_dim, interleaved, table, n_pos, positions, pos0, eps, dtype, false);
+    QkShape s;
+    if (!qk_shape(s, D, rot_dim, vec, dtype)) return DPCLIP_ERR_UNSUPPORTED;
+    cudaStream_t st = (cudaStream_t)stream;
+    return dtype == DPCLIP_F32 ? launch_qk<float>(p, s, false, st) : launch_qk<__nv_bfloat16>(p, s, false, st);
+}
+
+size_t dpclip_qknorm_workspace_bytes(int B, int T, int Hq, int Hk, int D) {
+    if (B <= 0 || T <= 0 || Hq < 0 || Hk < 0 || D <= 0) return kHeaderBytes;
+    return kHeaderBytes + round_up(sizeof(float) * (size_t)B * (qk_most_chunks(B, T, Hq) + qk_most_chunks(B, T, Hk)) * D, 256);
+}
+
+int dpclip_qknorm_backward(const dpclip_heads* parts, int n_parts, int B, int T, int D, int rot_dim, int interleaved,
+                           const float* table, long n_pos, const int* positions, long pos0, float eps, dpclip_dtype dtype,
+                           float* const* grads, float* const* sq_layers, void* workspace, size_t workspace_bytes, void* stream) {
+    int rc = qk_check(parts, n_parts, B, T, D, rot_dim, table, n_pos, positions, pos0, eps, dtype, true);
+    if (rc) return rc;
+    if (!grads || !sq_layers) return DPCLIP_ERR_INVALID_ARG;
+    for (int k = 0; k < n_parts; ++k)
+        if ((grads[k] && !is_aligned(grads[k], 4)) || (sq_layers[k] && !is_aligned(sq_layers[k], 4))) return DPCLIP_ERR_MISALIGNED;
+    QkParams p;
+    const bool vec = qk_fill(p, parts, n_parts, B, T, D, rot_dim, interleaved, table, n_pos, positions, pos0, eps, dtype, true);
+    QkShape s;
+    if (!qk_shape(s, D, rot_dim, vec, dtype)) return DPCLIP_ERR_UNSUPPORTED;
+    size_t chunks = 0;
+    for (int k = 0; k < n_parts; ++k) {
+        p.part[k].blocks = ceil_div(p.part[k].H, 32 / s.G);
+        if ((long)T * p.part[k].blocks > 0x3FFFFFFFL) return DPCLIP_ERR_UNSUPPORTED;
+        p.part[k].chunks = qk_chunks(B, (long)T * p.part[k].blocks);
+        chunks += p.part[k].chunks;
+    }
+    if (!workspace || !is_aligned(workspace, 16) || workspace_bytes < kHeaderBytes + sizeof(float) * B * chunks * D)
+        return DPCLIP_ERR_WORKSPACE;
+    p.part[0].part = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + kHeaderBytes);
+    p.part[1].part = p.part[0].part + (size_t)B * p.part[0].chunks * D;
+    cudaStream_t st = (cudaStream_t)stream;
+    rc = dtype == DPCLIP_F32 ? launch_qk<float>(p, s, true, st) : launch_qk<__nv_bfloat16>(p, s, true, st);
+    if (rc) return rc;
+    QkFinish f;
+    memset(&f, 0, sizeof(f));
+    f.D = D;
+    bool any = false;
+    for (int k = 0; k < n_parts; ++k) {
+        f.part[k] = p.part[k].part; f.chunks[k] = p.part[k].chunks; f.grads[k] = grads[k]; f.sq[k] = sq_layers[k];
+        any = any || grads[k] || sq_layers[k];
+    }
+    return any ? launch_after(qknorm_finish_kernel, dim3(B, n_parts), QK_THREADS, 0, st, f) : DPCLIP_OK;
+}
+
+}  // extern "C"

@@ -1,0 +1,52 @@
+// Clipped sums of stored per-example gradients: g[j] = sum_i clip[i] G[i][j] (+ noise), for parameters whose gradient an example's
+// norm kernel has left in memory (a few hundred numbers an example).
+//
+// CTA = 32 columns; its warps deal the examples among them with eight loads in flight, the warps' sums are added in order.  The bytes
+// are few (128 examples of 512 numbers: 256 KB), so what bounds it is the round trip of the loads.  32 warps where there are more than 256
+// examples.
+#pragma once
+#include "philox.cuh"
+
+namespace dpclip {
+
+struct StoredParams {
+    const float* G; long ld; int B, n;
+    const float* clip; float* g;
+    float noise_scale; uint32_t k0, k1, s0, s1;
+};
+
+template <int WARPS>
+__global__ void __launch_bounds__(32 * WARPS)
+stored_grad_kernel(const __grid_constant__ StoredParams p) {
+    constexpr int UNR = 8;
+    __shared__ float part[WARPS][32];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int c = blockIdx.x * 32 + lane;
+    float acc = 0.f;
+    if (c < p.n) {
+        for (int i = warp; i < p.B; i += WARPS * UNR) {
+            float v[UNR], f[UNR];
+#pragma unroll
+            for (int k = 0; k < UNR; ++k) {
+                const int e = i + k * WARPS;
+                v[k] = e < p.B ? __ldg(p.G + (size_t)e * p.ld + c) : 0.f;
+                f[k] = e < p.B ? (p.clip ? __ldg(p.clip + e) : 1.f) : 0.f;
+            }
+#pragma unroll
+            for (int k = 0; k < UNR; ++k) acc = fmaf(f[k], v[k], acc);
+        }
+    }
+    part[warp][lane] = acc;
+    __syncthreads();
+    if (warp != 0 || c >= p.n) return;
+#pragma unroll
+    for (int w = 1; w < WARPS; ++w) acc += part[w][lane];
+    if (p.noise_scale > 0.f) {
+        float z[4];
+        normals_at((size_t)(c & ~3), p.s0, p.s1, p.k0, p.k1, z);
+        acc = fmaf(p.noise_scale, (c & 2) ? ((c & 1) ? z[3] : z[2]) : ((c & 1) ? z[1] : z[0]), acc);
+    }
+    p.g[c] = acc;
+}
+
+}  // namespace dpclip
