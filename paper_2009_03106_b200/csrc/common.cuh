@@ -57,6 +57,28 @@ __device__ __forceinline__ float block_sum(float v, float* smem32) {
     return v;
 }
 
+// Two fp32 numbers in a register pair: sm_100a multiplies and adds pairs in one instruction, each half rounded as the scalar one is.
+struct f32x2 { unsigned long long v; };
+__device__ __forceinline__ f32x2 make_f32x2(float a, float b) { f32x2 r; asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(a), "f"(b)); return r; }
+__device__ __forceinline__ void split_f32x2(f32x2 p, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(p.v)); }
+__device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b) { f32x2 r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v)); return r; }
+__device__ __forceinline__ f32x2 sub2(f32x2 a, f32x2 b) { f32x2 r; asm("sub.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v)); return r; }
+__device__ __forceinline__ f32x2 mul2(f32x2 a, f32x2 b) { f32x2 r; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v)); return r; }
+__device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c) {
+    f32x2 r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+    return r;
+}
+__device__ __forceinline__ float sum_f32x2(f32x2 p) { float a, b; split_f32x2(p, a, b); return a + b; }
+// the two bf16 of a word
+__device__ __forceinline__ f32x2 bf16x2_to_f32x2(uint32_t w) { return make_f32x2(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u)); }
+__device__ __forceinline__ uint32_t f32x2_to_bf16x2(f32x2 p) {
+    float a, b;
+    split_f32x2(p, a, b);
+    const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&v);
+}
+
 // Range-checked build (-DDPCLIP_DEBUG, `python -m paper_2009_03106_b200.build --debug`): the stand-in for a
 // memory checker.  DPCLIP_IN_RANGE(i, n, status) is true when 0 <= i < n; otherwise it records
 // DPCLIP_ERR_RANGE in the workspace's status word and yields false, and the caller SKIPS the access -- no

@@ -38,27 +38,37 @@ bool fill_buckets(RbBuckets& r, const dpclip_relbias* c) {
         const long double border = r.exact * powl(ratio, (long double)k / m), whole = roundl(border);
         r.thr[k] = (int)(fabsl(border - whole) < 1e-12L * border ? whole : ceill(border));
     }
+    for (int b = 0; b < r.n_buckets; ++b) {
+        const int side = r.bidirectional && b >= r.n, c = b - (side ? r.n : 0);
+        const int from = c < r.exact ? c : r.thr[c - r.exact];
+        const int to = c < r.exact ? c : c + 1 < r.n ? r.thr[c - r.exact + 1] - 1 : RB_FAR;
+        r.lo[b] = side ? (from > 1 ? from : 1) : -to;
+        r.hi[b] = side ? to : (!r.bidirectional && c == 0 ? RB_FAR : -from);
+    }
     return true;
 }
 
-// A tile of the gradient: G groups of nr block rows by KT block columns, 256 threads.
-struct RbTiles { int E, nqb, nkb, KT, G, nr, qtiles, ktiles; };
+// A tile of the gradient: G groups of nr block rows by KT block columns.  64 threads where the rows have at most 64 blocks: a walk of such a
+// tile is then long enough to pay for the folds behind it (128 examples, 8 heads, 256 x 256, bf16: XX us, 256 threads YY).
+struct RbTiles { int E, threads, nqb, nkb, KT, G, nr, qtiles, ktiles; };
 RbTiles relbias_tiles(int B, int H, int Tq, int Tk, bool blocks8) {
     RbTiles t;
     t.E = blocks8 ? 8 : 1;
     t.nqb = ceil_div(Tq, t.E); t.nkb = ceil_div(Tk, t.E);
+    t.threads = t.nkb <= RB_FEW_THREADS ? RB_FEW_THREADS : RB_THREADS;
     const int most = blocks8 ? RB_THREADS : 4 * RB_THREADS;       // four walks a thread where a walk has one sum
     t.KT = t.nkb < most ? t.nkb : most;
     t.ktiles = ceil_div(t.nkb, t.KT);
-    t.G = RB_THREADS / t.KT;
+    t.G = t.threads / t.KT;
     if (t.G < 1) t.G = 1;
     if (t.G > t.nqb) t.G = t.nqb;
-    // long walks, as long as there are six CTAs an SM and 40 KB of shared memory hold the sums
+    // long walks, as long as there are CTAs enough for every SM and 40 KB of shared memory hold the sums
     const int longest = blocks8 ? 32 : 128;
+    const long ctas = t.threads == RB_THREADS ? 6L * kNumSMs : 12L * kNumSMs;
     t.nr = 1;
     auto fits = [&](int nr) { return (blocks8 ? rb_smem_floats<8>(t.KT, t.G, nr) : rb_smem_floats<1>(t.KT, t.G, nr)) * sizeof(float) <= 40 * 1024; };
     while (t.nr < longest && t.G * t.nr < t.nqb && fits(2 * t.nr) &&
-           (long)B * H * t.ktiles * ceil_div(t.nqb, (long)t.G * t.nr * 2) >= 6L * kNumSMs) t.nr *= 2;
+           ((long)t.ktiles * ceil_div(t.nqb, (long)t.G * t.nr * 2) * B * H >= ctas || (long)B * H * 2 >= ctas)) t.nr *= 2;
     // rows of single elements are walked eight at a time at least: fewer would be all set-up
     if (!blocks8) while (t.nr < 8 && t.G * t.nr < t.nqb) t.nr *= 2;
     t.qtiles = ceil_div(t.nqb, (long)t.G * t.nr);
@@ -71,9 +81,9 @@ inline size_t relbias_part_bytes(const RbTiles& t, int B, int H, int n_buckets) 
 template <typename T, int E>
 int launch_relbias_forward(RbForward& p, cudaStream_t st) {
     p.nqb = ceil_div(p.Tq, E); p.nkb = ceil_div(p.Tk, E);
-    // a walk of several block rows pays for its look-ups; at least 64 warps of walks an SM
+    // a walk of several block rows pays for its look-ups; one wave of four CTAs an SM
     const long blocks = (long)p.nqb * p.nkb * p.H;
-    p.nr = clamp_int(blocks / (kNumSMs * 64L * 32), 1, E == 1 ? 64 : 32);
+    p.nr = clamp_int((blocks + kNumSMs * 4L * RB_THREADS - 1) / (kNumSMs * 4L * RB_THREADS), 1, E == 1 ? 64 : 32);
     if (p.nr > p.nqb) p.nr = p.nqb;
     p.chunks = ceil_div(p.nqb, p.nr);
     p.items = (long)p.H * p.chunks * p.nkb;
@@ -84,9 +94,11 @@ int launch_relbias_forward(RbForward& p, cudaStream_t st) {
 }
 
 template <typename T, int E>
-int launch_relbias_grad(const RbGrad& p, cudaStream_t st) {
+int launch_relbias_grad(const RbGrad& p, int threads, cudaStream_t st) {
     const int smem = rb_smem_floats<E>(p.KT, p.G, p.nr) * (int)sizeof(float);
-    relbias_grad_kernel<T, E><<<(unsigned)((long)p.B * p.H * p.qtiles * p.ktiles), RB_THREADS, smem, st>>>(p);
+    const unsigned grid = (unsigned)((long)p.B * p.H * p.qtiles * p.ktiles);
+    if (threads == RB_THREADS) relbias_grad_kernel<T, E, RB_THREADS><<<grid, RB_THREADS, smem, st>>>(p);
+    else relbias_grad_kernel<T, E, RB_FEW_THREADS><<<grid, RB_FEW_THREADS, smem, st>>>(p);
     return finish_launch();
 }
 
@@ -105,32 +117,70 @@ bool qk_shape(QkShape& s, int D, int rot, bool vec, dpclip_dtype dtype) {
     return pairs <= 256;
 }
 
+// Calls of so many warp items (a token's block of heads) keep a ring of copies going in every warp; shorter ones are a chain of round trips
+// and take one item a warp.
+constexpr long kQkRingItems = 64L * kNumSMs;
+
+// The ring kernels' positions are 32-bit numbers: of the list, or t against a table moved by pos0.
+inline void qk_move_table(QkParams& p) {
+    if (!p.pos) {
+        const long first = p.pos0 < p.n_pos ? p.pos0 : p.n_pos;
+        if (p.table) p.table += first * p.rot;
+        p.n_pos -= first;
+    }
+    if (p.n_pos > 0x7FFFFFFFL) p.n_pos = 0x7FFFFFFFL;
+}
+
 template <typename T, int V, int NCH, int G>
 int launch_qk_forward(QkParams& p, cudaStream_t st) {
     for (int k = 0; k < 2; ++k) p.part[k].blocks = ceil_div(p.part[k].H, 32 / G);
     const long blocks = p.part[0].blocks + p.part[1].blocks, tokens = (long)p.B * p.T;
+    constexpr int WARPS = QK_THREADS / 32;
     if (blocks > 65535) return DPCLIP_ERR_UNSUPPORTED;
-    // four heads in flight a group where that leaves eight warps an SM, else one: short calls are a chain of round trips
-    constexpr int U = NCH == 1 ? 4 : 2;
-    const bool many = tokens * blocks / U >= 8L * kNumSMs;
-    const long warps = (tokens + (many ? U : 1) - 1) / (many ? U : 1);
-    const dim3 grid((unsigned)((warps * 32 + QK_THREADS - 1) / QK_THREADS), (unsigned)blocks);
-    if (many) qknorm_forward_kernel<T, V, NCH, G, U><<<grid, QK_THREADS, 0, st>>>(p);
-    else qknorm_forward_kernel<T, V, NCH, G, 1><<<grid, QK_THREADS, 0, st>>>(p);
+    if constexpr (V > 1) {
+        if (tokens * blocks >= kQkRingItems) {
+            // one wave of three CTAs an SM, every warp with as many tokens as any other
+            long x = 3L * kNumSMs / blocks;
+            if (x < 1) x = 1;
+            if (x > (tokens + WARPS - 1) / WARPS) x = (tokens + WARPS - 1) / WARPS;
+            const dim3 grid((unsigned)x, (unsigned)blocks);
+            qk_move_table(p);
+            if (p.interleaved) qknorm_forward_ring_kernel<T, V, G, true><<<grid, QK_THREADS, 0, st>>>(p);
+            else qknorm_forward_ring_kernel<T, V, G, false><<<grid, QK_THREADS, 0, st>>>(p);
+            return finish_launch();
+        }
+    }
+    const dim3 grid((unsigned)((tokens + WARPS - 1) / WARPS), (unsigned)blocks);
+    qknorm_forward_kernel<T, V, NCH, G, 1><<<grid, QK_THREADS, 0, st>>>(p);
     return finish_launch();
 }
+// Whether the backward pass of this shape keeps a ring of copies (its CTAs then have a block of heads each).
+inline bool qk_ring_backward(const QkShape& s, int B, int T, const QkPart* part) {
+    return s.V > 1 && T >= QK_THREADS / 32 * 4 && (long)B * T * (part[0].blocks + part[1].blocks) >= kQkRingItems;
+}
 template <typename T, int V, int NCH, int G>
-int launch_qk_backward(const QkParams& p, cudaStream_t st) {
+int launch_qk_backward(QkParams& p, bool ring, cudaStream_t st) {
+    constexpr int WARPS = QK_THREADS / 32;
+    if constexpr (V > 1) {
+        if (ring) {
+            constexpr int smem = WARPS * QK_BWD_STAGES * 4 * 512;      // 64 KB; the sums behind it need at most 16
+            const auto kernel = p.interleaved ? qknorm_backward_ring_kernel<T, V, G, true> : qknorm_backward_ring_kernel<T, V, G, false>;
+            if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return DPCLIP_ERR_CUDA;
+            const dim3 grid(p.part[0].blocks * p.part[0].chunks + p.part[1].blocks * p.part[1].chunks, p.B);
+            qk_move_table(p);
+            kernel<<<grid, QK_THREADS, smem, st>>>(p);
+            return finish_launch();
+        }
+    }
     constexpr int U = NCH <= 2 ? 2 : 1;
     const dim3 grid(p.part[0].chunks + p.part[1].chunks, p.B);
-    const size_t smem = sizeof(float) * (QK_THREADS / 32) * p.D;
-    qknorm_backward_kernel<T, V, NCH, G, U><<<grid, QK_THREADS, smem, st>>>(p);
+    qknorm_backward_kernel<T, V, NCH, G, U><<<grid, QK_THREADS, sizeof(float) * WARPS * p.D, st>>>(p);
     return finish_launch();
 }
 template <typename T>
-int launch_qk(QkParams& p, const QkShape& s, bool backward, cudaStream_t st) {
+int launch_qk(QkParams& p, const QkShape& s, bool backward, bool ring, cudaStream_t st) {
     constexpr int VV = sizeof(T) == 4 ? 4 : 8;
-#define DPCLIP_QK(V, NCH, G) return backward ? launch_qk_backward<T, V, NCH, G>(p, st) : launch_qk_forward<T, V, NCH, G>(p, st)
+#define DPCLIP_QK(V, NCH, G) return backward ? launch_qk_backward<T, V, NCH, G>(p, ring, st) : launch_qk_forward<T, V, NCH, G>(p, st)
     if (s.V == 1) switch (s.NCH) { case 1: DPCLIP_QK(1, 1, 32); case 2: DPCLIP_QK(1, 2, 32); case 4: DPCLIP_QK(1, 4, 32); default: DPCLIP_QK(1, 8, 32); }
     switch (s.G) {
         case 1: DPCLIP_QK(VV, 1, 1); case 2: DPCLIP_QK(VV, 1, 2); case 4: DPCLIP_QK(VV, 1, 4);
@@ -141,8 +191,14 @@ int launch_qk(QkParams& p, const QkShape& s, bool backward, cudaStream_t st) {
 
 // CTAs an example for `items` warp items of one part: about four CTAs an SM in all, at least sixteen items a CTA
 inline int qk_chunks(int B, long items) { return clamp_int(ceil_div(4L * kNumSMs, B), 1, items / 16 > 0 ? items / 16 : 1); }
-// most chunks any form of the kernels makes, for the workspace: one head a warp item
-inline int qk_most_chunks(int B, int T, int H) { return H > 0 ? qk_chunks(B, (long)T * H) : 0; }
+// most partial sums an example any form of the kernels makes, for the workspace: one head a warp item without a ring; with one at most
+// H blocks of T / 64 chunks, and no more than its rule asks for
+inline long qk_most_sums(int B, int T, int H) {
+    if (H <= 0) return 0;
+    const long plain = qk_chunks(B, (long)T * H), chunks = clamp_int(4L * kNumSMs / B, 1, T / 64 > 0 ? T / 64 : 1);
+    const long ring = chunks * H < 4L * kNumSMs / B + H ? chunks * H : 4L * kNumSMs / B + H;
+    return plain > ring ? plain : ring;
+}
 
 int qk_check(const dpclip_heads* parts, int n_parts, int B, int T, int D, int rot_dim, const float* table, long n_pos,
              const int* positions, long pos0, float eps, dpclip_dtype dtype, bool backward) {
@@ -263,8 +319,8 @@ int dpclip_relbias_sqnorms(const void* dS, long ld, long head_stride, long examp
     p.part = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + kHeaderBytes);
     cudaStream_t st = (cudaStream_t)stream;
     int rc;
-    if (dtype == DPCLIP_F32) rc = vec ? launch_relbias_grad<float, 8>(p, st) : launch_relbias_grad<float, 1>(p, st);
-    else rc = vec ? launch_relbias_grad<__nv_bfloat16, 8>(p, st) : launch_relbias_grad<__nv_bfloat16, 1>(p, st);
+    if (dtype == DPCLIP_F32) rc = vec ? launch_relbias_grad<float, 8>(p, t.threads, st) : launch_relbias_grad<float, 1>(p, t.threads, st);
+    else rc = vec ? launch_relbias_grad<__nv_bfloat16, 8>(p, t.threads, st) : launch_relbias_grad<__nv_bfloat16, 1>(p, t.threads, st);
     if (rc) return rc;
     int lanes = 1;
     while (lanes < 32 && lanes < tiles) lanes *= 2;
@@ -290,12 +346,12 @@ int dpclip_qknorm_forward(const dpclip_heads* parts, int n_parts, int B, int T, 
     QkShape s;
     if (!qk_shape(s, D, rot_dim, vec, dtype)) return DPCLIP_ERR_UNSUPPORTED;
     cudaStream_t st = (cudaStream_t)stream;
-    return dtype == DPCLIP_F32 ? launch_qk<float>(p, s, false, st) : launch_qk<__nv_bfloat16>(p, s, false, st);
+    return dtype == DPCLIP_F32 ? launch_qk<float>(p, s, false, false, st) : launch_qk<__nv_bfloat16>(p, s, false, false, st);
 }
 
 size_t dpclip_qknorm_workspace_bytes(int B, int T, int Hq, int Hk, int D) {
     if (B <= 0 || T <= 0 || Hq < 0 || Hk < 0 || D <= 0) return kHeaderBytes;
-    return kHeaderBytes + round_up(sizeof(float) * (size_t)B * (qk_most_chunks(B, T, Hq) + qk_most_chunks(B, T, Hk)) * D, 256);
+    return kHeaderBytes + round_up(sizeof(float) * (size_t)B * (qk_most_sums(B, T, Hq) + qk_most_sums(B, T, Hk)) * D, 256);
 }
 
 int dpclip_qknorm_backward(const dpclip_heads* parts, int n_parts, int B, int T, int D, int rot_dim, int interleaved,
@@ -310,26 +366,36 @@ int dpclip_qknorm_backward(const dpclip_heads* parts, int n_parts, int B, int T,
     const bool vec = qk_fill(p, parts, n_parts, B, T, D, rot_dim, interleaved, table, n_pos, positions, pos0, eps, dtype, true);
     QkShape s;
     if (!qk_shape(s, D, rot_dim, vec, dtype)) return DPCLIP_ERR_UNSUPPORTED;
-    size_t chunks = 0;
+    size_t sums[2] = {0, 0};                               // partial sums an example
     for (int k = 0; k < n_parts; ++k) {
         p.part[k].blocks = ceil_div(p.part[k].H, 32 / s.G);
         if ((long)T * p.part[k].blocks > 0x3FFFFFFFL) return DPCLIP_ERR_UNSUPPORTED;
-        p.part[k].chunks = qk_chunks(B, (long)T * p.part[k].blocks);
-        chunks += p.part[k].chunks;
     }
-    if (!workspace || !is_aligned(workspace, 16) || workspace_bytes < kHeaderBytes + sizeof(float) * B * chunks * D)
+    const bool ring = qk_ring_backward(s, B, T, p.part);
+    for (int k = 0; k < n_parts; ++k) {
+        QkPart& q = p.part[k];
+        if (ring) {
+            // about two waves of two CTAs an SM, at least 64 positions a CTA
+            q.chunks = clamp_int(4L * kNumSMs / ((long)B * (p.part[0].blocks + p.part[1].blocks)), 1, T / 64 > 0 ? T / 64 : 1);
+            sums[k] = (size_t)q.blocks * q.chunks;
+        } else {
+            q.chunks = qk_chunks(B, (long)T * q.blocks);
+            sums[k] = q.chunks;
+        }
+    }
+    if (!workspace || !is_aligned(workspace, 16) || workspace_bytes < kHeaderBytes + sizeof(float) * B * (sums[0] + sums[1]) * D)
         return DPCLIP_ERR_WORKSPACE;
     p.part[0].part = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + kHeaderBytes);
-    p.part[1].part = p.part[0].part + (size_t)B * p.part[0].chunks * D;
+    p.part[1].part = p.part[0].part + B * sums[0] * D;
     cudaStream_t st = (cudaStream_t)stream;
-    rc = dtype == DPCLIP_F32 ? launch_qk<float>(p, s, true, st) : launch_qk<__nv_bfloat16>(p, s, true, st);
+    rc = dtype == DPCLIP_F32 ? launch_qk<float>(p, s, true, ring, st) : launch_qk<__nv_bfloat16>(p, s, true, ring, st);
     if (rc) return rc;
     QkFinish f;
     memset(&f, 0, sizeof(f));
     f.D = D;
     bool any = false;
     for (int k = 0; k < n_parts; ++k) {
-        f.part[k] = p.part[k].part; f.chunks[k] = p.part[k].chunks; f.grads[k] = grads[k]; f.sq[k] = sq_layers[k];
+        f.part[k] = p.part[k].part; f.chunks[k] = (int)sums[k]; f.grads[k] = grads[k]; f.sq[k] = sq_layers[k];
         any = any || grads[k] || sq_layers[k];
     }
     return any ? launch_after(qknorm_finish_kernel, dim3(B, n_parts), QK_THREADS, 0, st, f) : DPCLIP_OK;

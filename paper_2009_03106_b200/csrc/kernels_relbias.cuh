@@ -14,18 +14,23 @@
 //                            every element is read once, those behind a length or above the causal diagonal not at all.
 //   relbias_finish_kernel  : adds up the tiles of an example and takes the squared norm over buckets and heads.
 #pragma once
+#include <type_traits>
+
 #include "common.cuh"
 
 namespace dpclip {
 
-constexpr int RB_THREADS = 256;
+constexpr int RB_THREADS = 256;          // forward pass, and gradients whose tiles are wide
+constexpr int RB_FEW_THREADS = 64;       // gradients of short rows
 constexpr int RB_MAX_BUCKETS = 256;
+constexpr int RB_FAR = 1 << 30;
 
 // Distances to buckets.  Per direction `n` buckets: distances below `exact` have one each, those beyond share the others on a
 // logarithmic scale; thr[k] is the smallest distance of bucket exact + k.
 struct RbBuckets {
     int n_buckets, n, exact, max_distance, bidirectional, causal;
     int thr[RB_MAX_BUCKETS];
+    int lo[RB_MAX_BUCKETS], hi[RB_MAX_BUCKETS];      // the distances of every bucket, empty where lo > hi; RB_FAR: no end
 };
 
 __host__ __device__ inline int rb_bucket(const RbBuckets& r, long rel) {
@@ -35,21 +40,10 @@ __host__ __device__ inline int rb_bucket(const RbBuckets& r, long rel) {
     if (r.bidirectional) { base = x > 0 ? r.n : 0; d = x > 0 ? x : -x; }
     else d = x < 0 ? -x : 0;
     if (d < r.exact) return base + d;
+    if (d >= r.max_distance) return base + r.n - 1;
     int lo = 0, hi = r.n - r.exact - 1;                                  // the last k with thr[k] <= d
     while (lo < hi) { const int mid = (lo + hi + 1) >> 1; if (r.thr[mid] <= d) lo = mid; else hi = mid - 1; }
     return base + r.exact + lo;
-}
-
-// the distances key - query of bucket b: [lo, hi], empty when lo > hi
-__device__ __forceinline__ void rb_interval(const RbBuckets& r, int b, long& lo, long& hi) {
-    constexpr long FAR = 1L << 40;
-    const int side = r.bidirectional && b >= r.n;
-    const int c = b - (side ? r.n : 0);
-    long dlo, dhi;
-    if (c < r.exact) { dlo = c; dhi = c; }
-    else { dlo = r.thr[c - r.exact]; dhi = c + 1 < r.n ? (long)r.thr[c - r.exact + 1] - 1 : FAR; }
-    if (side) { lo = dlo > 1 ? dlo : 1; hi = dhi; }
-    else { lo = -dhi; hi = (!r.bidirectional && c == 0) ? FAR : -dlo; }
 }
 
 // ------------------------------------------------------------------------------------------------ forward
@@ -69,7 +63,7 @@ __device__ __forceinline__ void rb_store(float* p, float v) { *p = v; }
 __device__ __forceinline__ void rb_store(__nv_bfloat16* p, float v) { *p = __float2bfloat16_rn(v); }
 
 template <typename T, int E>
-__global__ void __launch_bounds__(RB_THREADS)
+__global__ void __launch_bounds__(RB_THREADS, 4)
 relbias_forward_kernel(const __grid_constant__ RbForward p) {
     const long item = (long)blockIdx.x * RB_THREADS + threadIdx.x;
     if (item >= p.items) return;
@@ -90,7 +84,9 @@ relbias_forward_kernel(const __grid_constant__ RbForward p) {
         };
         if (E > 1) {
             const long last = first + 2 * E - 2;
-            if ((first > 0) == (last > 0) && rb_bucket(p.r, first) == rb_bucket(p.r, last)) {
+            // beyond max_distance on one side there is one bucket, and no search for it
+            if (first >= p.r.max_distance || last <= -p.r.max_distance ||
+                ((first > 0) == (last > 0) && rb_bucket(p.r, first) == rb_bucket(p.r, last))) {
                 const float x = value(first);
 #pragma unroll
                 for (int j = 0; j < 2 * E - 1; ++j) v[j] = x;
@@ -155,75 +151,142 @@ struct RbGrad {
 
 template <int E>
 __host__ __device__ constexpr int rb_smem_floats(int KT, int G, int nr) {
-    return G * (KT + nr - 1) * (2 * E - 1) + E * (KT + G * nr);
+    return (E > 1 ? 2 : 1) * G * E * (KT + nr) + E * (KT + G * nr);
 }
 
-__device__ __forceinline__ float rb_word(uint32_t w, int half) { return __uint_as_float(half ? w & 0xFFFF0000u : w << 16); }
-
-// Block rows [0, E) x columns [0, E) at `at`: acc[E - 1 + j - i] += element (i, j) where (i, j) counts.
-template <typename T, int E>
-__device__ __forceinline__ void rb_add_block(const T* at, long ld, int rows, int cols, bool can_load, float (&acc)[2 * E - 1], int causal_from) {
-    // element (i, j) counts when i < rows, j < cols and j - i <= causal_from
-    if (rows >= E && cols >= E && causal_from >= E - 1) {
-        if constexpr (sizeof(T) == 2) {
-            uint4 x[E];
+// The sums along the 2E - 1 diagonals of a thread's blocks.  E = 8: element (i, j) belongs to diagonal 7 + j - i, and neighbours of a row are
+// added as a pair: those of even rows to the pairs that start at odd diagonals, those of odd rows to the ones that start at even diagonals.
+template <int E> struct RbSums {
+    float s;
+    __device__ __forceinline__ void clear() { s = 0.f; }
+    __device__ __forceinline__ void write(float* to, int) const { to[0] = s; }
+};
+template <> struct RbSums<8> {
+    f32x2 odd[7], even[7];               // odd[k]: diagonals 2k + 1, 2k + 2;  even[k]: 2k, 2k + 1
+    __device__ __forceinline__ void clear() {
 #pragma unroll
-            for (int i = 0; i < E; ++i) x[i] = __ldg(reinterpret_cast<const uint4*>(at + i * ld));
-#pragma unroll
-            for (int i = 0; i < E; ++i) {
-                const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
-#pragma unroll
-                for (int j = 0; j < E; ++j) acc[E - 1 + j - i] += rb_word(w[j >> 1], j & 1);
-            }
-        } else {
-#pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                float4 x[E];
-#pragma unroll
-                for (int i = 0; i < E / 2; ++i) {
-                    const float4* row = reinterpret_cast<const float4*>(at + (half * (E / 2) + i) * ld);
-                    x[2 * i] = __ldg(row); x[2 * i + 1] = __ldg(row + 1);
-                }
-#pragma unroll
-                for (int i = 0; i < E / 2; ++i) {
-                    const float e[8] = {x[2 * i].x, x[2 * i].y, x[2 * i].z, x[2 * i].w, x[2 * i + 1].x, x[2 * i + 1].y, x[2 * i + 1].z, x[2 * i + 1].w};
-#pragma unroll
-                    for (int j = 0; j < E; ++j) acc[E - 1 + j - (half * (E / 2) + i)] += e[j];
-                }
-            }
-        }
-        return;
+        for (int k = 0; k < 7; ++k) odd[k] = even[k] = make_f32x2(0.f, 0.f);
     }
-    // an edge: what does not count may be anything, NaN too, so it is left out, not multiplied by zero
+    // elements 2m and 2m + 1 of row i
+    template <int I, int M> __device__ __forceinline__ void add(f32x2 x) {
+        constexpr int d = 7 + 2 * M - I;
+        if constexpr (d & 1) odd[d >> 1] = add2(odd[d >> 1], x);
+        else even[d >> 1] = add2(even[d >> 1], x);
+    }
+    template <int I> __device__ __forceinline__ void add_row(f32x2 a, f32x2 b, f32x2 c, f32x2 d) {
+        add<I, 0>(a); add<I, 1>(b); add<I, 2>(c); add<I, 3>(d);
+    }
+    // diagonals 0 .. 7 to to[0 .. 7], 8 .. 14 to to[other + 8 ..]: neighbours' walks share distances, not places
+    __device__ __forceinline__ void write(float* to, int other) const {
+        float o[14], e[14], d[16];
 #pragma unroll
-    for (int i = 0; i < E; ++i) {
-        if (i >= rows) break;
-        const T* row = at + i * ld;
-        float e[E];
-        if (can_load) {
-            if constexpr (sizeof(T) == 2) {
-                const uint4 x = __ldg(reinterpret_cast<const uint4*>(row));
-                const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+        for (int k = 0; k < 7; ++k) { split_f32x2(odd[k], o[2 * k], o[2 * k + 1]); split_f32x2(even[k], e[2 * k], e[2 * k + 1]); }
+        d[0] = e[0];
 #pragma unroll
-                for (int j = 0; j < E; ++j) e[j] = rb_word(w[j >> 1], j & 1);
-            } else {
-                const float4 x = __ldg(reinterpret_cast<const float4*>(row)), y = __ldg(reinterpret_cast<const float4*>(row) + 1);
-                e[0] = x.x; e[1] = x.y; e[2] = x.z; e[3] = x.w; e[4] = y.x; e[5] = y.y; e[6] = y.z; e[7] = y.w;
-            }
-        } else {
+        for (int k = 1; k < 14; ++k) d[k] = o[k - 1] + e[k];
+        d[14] = o[13];
+        d[15] = 0.f;
 #pragma unroll
-            for (int j = 0; j < E; ++j) e[j] = j < cols ? to_f32(row[j]) : 0.f;
+        for (int k = 0; k < 16; k += 4) *reinterpret_cast<float4*>(to + k + (k >= 8 ? other : 0)) = make_float4(d[k], d[k + 1], d[k + 2], d[k + 3]);
+    }
+};
+template <typename T> struct RbRow;      // eight elements of a row as loaded
+template <> struct RbRow<__nv_bfloat16> {
+    uint4 x;
+    __device__ __forceinline__ void load(const __nv_bfloat16* p) { x = __ldg(reinterpret_cast<const uint4*>(p)); }
+    __device__ __forceinline__ void pairs(f32x2 (&e)[4]) const {
+        e[0] = bf16x2_to_f32x2(x.x); e[1] = bf16x2_to_f32x2(x.y); e[2] = bf16x2_to_f32x2(x.z); e[3] = bf16x2_to_f32x2(x.w);
+    }
+};
+template <> struct RbRow<float> {
+    float4 x, y;
+    __device__ __forceinline__ void load(const float* p) { x = __ldg(reinterpret_cast<const float4*>(p)); y = __ldg(reinterpret_cast<const float4*>(p) + 1); }
+    __device__ __forceinline__ void pairs(f32x2 (&e)[4]) const {
+        e[0] = make_f32x2(x.x, x.y); e[1] = make_f32x2(x.z, x.w); e[2] = make_f32x2(y.x, y.y); e[3] = make_f32x2(y.z, y.w);
+    }
+};
+
+// N rows of a block from row I on, 128 bytes a thread: loaded as one, added as one.
+template <typename T> constexpr int RB_ROWS = sizeof(T) == 2 ? 8 : 4;
+template <typename T> struct RbRows {
+    RbRow<T> x[RB_ROWS<T>];
+    __device__ __forceinline__ void load(const T* at, long ld) {
+#pragma unroll
+        for (int i = 0; i < RB_ROWS<T>; ++i) x[i].load(at + i * ld);
+    }
+    template <int I> __device__ __forceinline__ void add(RbSums<8>& acc) const {
+        f32x2 e[4];
+        auto row = [&](auto k) {
+            constexpr int i = decltype(k)::value;
+            if constexpr (i < RB_ROWS<T>) { x[i].pairs(e); acc.template add_row<I + i>(e[0], e[1], e[2], e[3]); }
+        };
+        row(std::integral_constant<int, 0>()); row(std::integral_constant<int, 1>()); row(std::integral_constant<int, 2>()); row(std::integral_constant<int, 3>());
+        row(std::integral_constant<int, 4>()); row(std::integral_constant<int, 5>()); row(std::integral_constant<int, 6>()); row(std::integral_constant<int, 7>());
+    }
+};
+// n blocks along the diagonal, all of whose elements count: the next 128 bytes are under way while the last are added.
+template <typename T>
+__device__ __forceinline__ void rb_add_full(const T* at, long ld, int n, RbSums<8>& acc) {
+    const long step = 8 * ld + 8;
+    RbRows<T> a, b;
+    a.load(at, ld);
+    if constexpr (sizeof(T) == 2) {
+        int i = 0;
+        for (; i + 2 <= n; i += 2) {
+            b.load(at + step, ld);
+            a.template add<0>(acc);
+            at += 2 * step;
+            if (i + 2 < n) a.load(at, ld);
+            b.template add<0>(acc);
         }
-#pragma unroll
-        for (int j = 0; j < E; ++j) acc[E - 1 + j - i] += j < cols && j - i <= causal_from ? e[j] : 0.f;
+        if (i < n) a.template add<0>(acc);
+    } else {
+        for (int i = 0; i < n; ++i) {
+            b.load(at + 4 * ld, ld);
+            a.template add<0>(acc);
+            at += step;
+            if (i + 1 < n) a.load(at, ld);
+            b.template add<4>(acc);
+        }
     }
 }
+// Row I of a block at an edge: element j counts when j < cols and j - I <= causal_from.  What does not count may be anything, NaN too, so it
+// is left out, not multiplied by zero.
+template <typename T, int I>
+__device__ __forceinline__ void rb_add_edge_row(const T* row, int rows, int cols, bool can_load, int causal_from, RbSums<8>& acc) {
+    if (I >= rows) return;
+    float e[8];
+    if (can_load) {
+        RbRow<T> x;
+        f32x2 w[4];
+        x.load(row);
+        x.pairs(w);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) split_f32x2(w[k], e[2 * k], e[2 * k + 1]);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) e[j] = j < cols ? to_f32(row[j]) : 0.f;
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) e[j] = j < cols && j - I <= causal_from ? e[j] : 0.f;
+    acc.template add_row<I>(make_f32x2(e[0], e[1]), make_f32x2(e[2], e[3]), make_f32x2(e[4], e[5]), make_f32x2(e[6], e[7]));
+}
+template <typename T>
+__device__ __forceinline__ void rb_add_edge(const T* at, long ld, int rows, int cols, bool can_load, RbSums<8>& acc, int causal_from) {
+    rb_add_edge_row<T, 0>(at, rows, cols, can_load, causal_from, acc);
+    rb_add_edge_row<T, 1>(at + ld, rows, cols, can_load, causal_from, acc);
+    rb_add_edge_row<T, 2>(at + 2 * ld, rows, cols, can_load, causal_from, acc);
+    rb_add_edge_row<T, 3>(at + 3 * ld, rows, cols, can_load, causal_from, acc);
+    rb_add_edge_row<T, 4>(at + 4 * ld, rows, cols, can_load, causal_from, acc);
+    rb_add_edge_row<T, 5>(at + 5 * ld, rows, cols, can_load, causal_from, acc);
+    rb_add_edge_row<T, 6>(at + 6 * ld, rows, cols, can_load, causal_from, acc);
+    rb_add_edge_row<T, 7>(at + 7 * ld, rows, cols, can_load, causal_from, acc);
+}
 
-template <typename T, int E>
-__global__ void __launch_bounds__(RB_THREADS)
+template <typename T, int E, int THREADS>
+__global__ void __launch_bounds__(THREADS, 512 / THREADS)
 relbias_grad_kernel(const __grid_constant__ RbGrad p) {
-    constexpr int W = 2 * E - 1;
-    extern __shared__ float rb_smem[];
+    extern __shared__ __align__(16) float rb_smem[];
     const int tid = threadIdx.x;
     const int tiles = p.qtiles * p.ktiles;
     const long bh = (long)blockIdx.x / tiles;
@@ -236,17 +299,20 @@ relbias_grad_kernel(const __grid_constant__ RbGrad p) {
     // nothing of the tile counts: behind a length, or all keys behind the tile's last query
     const long q_last = min((long)ql, (long)E * (qb0 + p.G * p.nr)) - 1;
     if ((long)E * qb0 >= ql || (long)E * kb0 >= kl || (p.r.causal && (long)E * kb0 > q_last + p.off)) {
-        for (int i = tid; i < p.r.n_buckets; i += RB_THREADS) out[i] = 0.f;
+        for (int i = tid; i < p.r.n_buckets; i += THREADS) out[i] = 0.f;
         return;
     }
-    const int dpg = p.KT + p.nr - 1;                    // diagonals of blocks a group
-    float* const diag = rb_smem;                        // [G][dpg][W]
-    float* const line = rb_smem + p.G * dpg * W;        // [E * (KT + G * nr)]
-    for (int i = tid; i < p.G * dpg * W; i += RB_THREADS) diag[i] = 0.f;
+    // sums of the walks by distance, a group at a time: a walk on block diagonal d (from -(nr - 1)) has distances E d .. E d + 2E - 2 of the
+    // group's; E > 1: its lower and upper half go to two arrays, where no other walk writes
+    const int span = E * (p.KT + p.nr);
+    float* const diag = rb_smem;                                        // [E > 1 ? 2 : 1][G][span]
+    const int other = p.G * span;
+    float* const line = diag + (E > 1 ? 2 : 1) * other;                 // [E * (KT + G * nr)]
+    for (int i = tid; i < (E > 1 ? 2 : 1) * other; i += THREADS) diag[i] = 0.f;
     __syncthreads();
 
     const T* const plane = static_cast<const T*>(p.dS) + (long)b * p.bs + (long)h * p.hs;
-    for (int slot = tid; slot < p.G * p.KT; slot += RB_THREADS) {
+    for (int slot = tid; slot < p.G * p.KT; slot += THREADS) {
         const int g = slot / p.KT, c = slot - g * p.KT;
         if (c >= ncol) continue;
         const int row0 = qb0 + g * p.nr;
@@ -254,9 +320,8 @@ relbias_grad_kernel(const __grid_constant__ RbGrad p) {
         int s = 0, col = c;
         while (s < steps) {
             const int end = min(steps, s + ncol - col);
-            float acc[W];
-#pragma unroll
-            for (int j = 0; j < W; ++j) acc[j] = 0.f;
+            RbSums<E> acc;
+            acc.clear();
             const int delta = col - s;                  // block diagonal of the walk, -(nr - 1) .. KT - 1
             // key - query at the blocks' first element
             const long rel = (long)E * ((kb0 + col) - (row0 + s)) - p.off;
@@ -267,46 +332,52 @@ relbias_grad_kernel(const __grid_constant__ RbGrad p) {
                 if constexpr (E == 1) {
                     const int n = min(end - s, min(ql - (row0 + s), kl - (kb0 + col)));
 #pragma unroll 8
-                    for (int i = 0; i < n; ++i) { acc[0] += to_f32(*at); at += p.ld + 1; }
+                    for (int i = 0; i < n; ++i) { acc.s += to_f32(*at); at += p.ld + 1; }
                 } else {
-                    for (int i = s; i < end; ++i, at += (long)E * p.ld + E) {
+                    // blocks that are inside the lengths come first on a walk
+                    const int full = cf < E - 1 ? 0 : max(0, min(end - s, min(ql / E - (row0 + s), kl / E - (kb0 + col))));
+                    if (full > 0) rb_add_full<T>(at, p.ld, full, acc);
+                    at += full * ((long)E * p.ld + E);
+                    for (int i = s + full; i < end; ++i, at += (long)E * p.ld + E) {
                         const int q0 = E * (row0 + i), k0 = E * (kb0 + col + i - s);
                         if (k0 >= kl) break;
-                        rb_add_block<T, E>(at, p.ld, ql - q0, kl - k0, k0 + E <= p.Tk, acc, cf);
+                        rb_add_edge<T>(at, p.ld, ql - q0, kl - k0, k0 + E <= p.Tk, acc, cf);
                     }
                 }
             }
-            float* to = diag + ((size_t)g * dpg + (delta + p.nr - 1)) * W;
-#pragma unroll
-            for (int j = 0; j < W; ++j) to[j] = acc[j];
+            acc.write(diag + g * span + E * (delta + p.nr - 1), other);
             s = end; col = 0;
         }
     }
     __syncthreads();
     // one sum a distance: distance x - (E * (qb0 + G * nr) - 1) + E * kb0 - off
     const int X = E * (p.KT + p.G * p.nr) - 1;
-    for (int x = tid; x < X; x += RB_THREADS) {
+    for (int x = tid; x < X; x += THREADS) {
         float a = 0.f;
-        for (int g = 0; g < p.G; ++g) {
-            const int y = x - E * (p.G - 1 - g) * p.nr;
-            if (y < 0) continue;
-            const int d = y / E, e = y - d * E;
-            if (d < dpg) a += diag[((size_t)g * dpg + d) * W + e];
-            if (e < E - 1 && d >= 1 && d - 1 < dpg) a += diag[((size_t)g * dpg + d - 1) * W + e + E];
+        int at = x - E * (p.G - 1) * p.nr;
+        for (int g = 0; g < p.G; ++g, at += E * p.nr) {
+            if (at < 0 || at >= span) continue;
+            a += diag[g * span + at];
+            if (E > 1) a += diag[other + g * span + at];
         }
         line[x] = a;
     }
     __syncthreads();
+    // eight lanes a bucket
     const long rel0 = (long)E * kb0 - ((long)E * (qb0 + p.G * p.nr) - 1) - p.off;
-    const int warp = tid >> 5, lane = tid & 31;
-    for (int k = warp; k < p.r.n_buckets; k += RB_THREADS / 32) {
-        long lo, hi;
-        rb_interval(p.r, k, lo, hi);
-        lo = max(lo - rel0, 0L); hi = min(hi - rel0, (long)X - 1);
+    const int sub = tid & 7;
+    for (int k0 = 0; k0 < p.r.n_buckets; k0 += THREADS / 8) {
+        const int k = k0 + (tid >> 3);
         float a = 0.f;
-        for (long x = lo + lane; x <= hi; x += 32) a += line[x];
-        a = warp_sum(a);
-        if (lane == 0) out[k] = a;
+        if (k < p.r.n_buckets) {
+            const int lo = p.r.lo[k] == -RB_FAR ? 0 : (int)min(max(p.r.lo[k] - rel0, 0L), (long)X);
+            const int hi = p.r.hi[k] == RB_FAR ? X - 1 : (int)max(min(p.r.hi[k] - rel0, (long)X - 1), -1L);
+            for (int x = lo + sub; x <= hi; x += 8) a += line[x];
+        }
+        a += __shfl_xor_sync(0xFFFFFFFFu, a, 1);
+        a += __shfl_xor_sync(0xFFFFFFFFu, a, 2);
+        a += __shfl_xor_sync(0xFFFFFFFFu, a, 4);
+        if (k < p.r.n_buckets && sub == 0) out[k] = a;
     }
 }
 
