@@ -584,6 +584,28 @@ size_t dpclip_qknorm_workspace_bytes(int B, int T, int Hq, int Hk, int D);
 /* Angles of n_pos positions: pos * base^(-2 i / rot_dim) / scale, computed in 64 bits. */
 int dpclip_rotation_table(float* table, long n_pos, int rot_dim, double base, double scale, void* stream);
 
+/* Gated feed-forward block, both projections, the activation and the product in one pass:
+ *   Zg = X Wg^T + bg,  Zu = X Wu^T + bu,  H = act(Zg) (.) Zu.
+ * Gate and up rows are ONE weight W [2F][K] (gate rows first), as dZ = [dZg dZu] is ONE signal [M][2F]: with Layer (A = X, Zbar = dZ, d_in =
+ * K, d_out = 2F) the step's norms and clipped sums of both projections are those of a single dense layer.
+ *   X  [M][K] row stride ldx;  W [2F][K] row stride ldw;  bias [2F] fp32 or NULL;  H [M][F] row stride ldh, OVERWRITTEN
+ *   Z  [M][2F] row stride ldz, OVERWRITTEN with the pre-activations (for the backward pass), or NULL
+ * X, W, H, Z of one `dtype`; products are summed in fp32, H comes from the unrounded Z.  bf16 runs on the tensor cores (rows that are no
+ * 16-byte multiples are laid out in the workspace first, or stay on the fp32 ALUs where that costs more), fp32 on the fp32 ALUs.  M from 1
+ * (one token: the weights are streamed once).  Outputs may not overlap inputs.
+ *   workspace >= dpclip_gated_workspace_bytes(), its header set up by dpclip_workspace_init
+ * Errors: INVALID_ARG, MISALIGNED, WORKSPACE. */
+typedef enum { DPCLIP_ACT_SILU = 0, DPCLIP_ACT_GELU = 1, DPCLIP_ACT_GELU_TANH = 2, DPCLIP_ACT_RELU = 3 } dpclip_activation;
+int dpclip_gated_forward(const void* X, long ldx, const void* W, long ldw, const float* bias, int M, int K, int F, dpclip_dtype dtype,
+                         dpclip_activation act, void* H, long ldh, void* Z, long ldz, void* workspace, size_t workspace_bytes, void* stream);
+/* From dH: dZg = dH (.) Zu (.) act'(Zg), dZu = dH (.) act(Zg) and, unless dX is NULL, dX = dZ W.
+ *   dZ  [M][2F], OVERWRITTEN; may be Z itself (same stride).  dX [M][K] or NULL (then W and the workspace may be NULL)
+ * relu' is 0 at 0.  dX is the product with dZ as stored. */
+int dpclip_gated_backward(const void* dH, long lddh, const void* Z, long ldz, const void* W, long ldw, int M, int K, int F,
+                          dpclip_dtype dtype, dpclip_activation act, void* dZ, long lddz, void* dX, long lddx,
+                          void* workspace, size_t workspace_bytes, void* stream);
+size_t dpclip_gated_workspace_bytes(int M, int K, int F, dpclip_dtype dtype);
+
 /* Number of kernels this library has launched in this process (a host-side
  * counter for benchmarks and tests; cudaMemset calls are not counted, nor is the
  * kernel that stands for them in a step on several streams). */

@@ -11,6 +11,7 @@ from .binding import (  # noqa: F401
     dpclip_layer_sqnorms, dpclip_pick_method, dpclip_read_status, dpclip_status_string,
     dpclip_gram_layers_sqnorms, dpclip_same_shape_layers_clipped_grad_noise, dpclip_step, dpclip_step_workspace_bytes, dpclip_step_streams, dpclip_model_step_streams, dpclip_step_lanes, dpclip_model_step_lanes, dpclip_step_side_workspace_bytes, dpclip_model_side_workspace_bytes, dpclip_step_host, dpclip_step_noise, dpclip_step_per_layer, dpclip_t1_layers_clipped_grad_noise, dpclip_t1_layers_sqnorms, dpclip_t1_layers_supported, dpclip_version, dpclip_workspace_bytes, dpclip_workspace_init,
     dpclip_stored_clipped_grad, dpclip_relbias_bucket, dpclip_relbias_forward, dpclip_relbias_sqnorms, dpclip_relbias_workspace_bytes,
+    DPCLIP_ACT_GELU, DPCLIP_ACT_GELU_TANH, DPCLIP_ACT_RELU, DPCLIP_ACT_SILU, dpclip_gated_backward, dpclip_gated_forward, dpclip_gated_workspace_bytes,
     dpclip_rotation_table, dpclip_qknorm_forward, dpclip_qknorm_backward, dpclip_qknorm_workspace_bytes,
     library_path, load_library,
 )

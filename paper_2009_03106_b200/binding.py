@@ -20,6 +20,7 @@ _LIB_PATH = os.environ.get("DPCLIP_LIBRARY") or os.path.join(_HERE, "libdpclip.s
 _lib = None
 
 DPCLIP_F32, DPCLIP_BF16 = 0, 1
+DPCLIP_ACT_SILU, DPCLIP_ACT_GELU, DPCLIP_ACT_GELU_TANH, DPCLIP_ACT_RELU = 0, 1, 2, 3
 DPCLIP_AUTO, DPCLIP_T1, DPCLIP_GRAM, DPCLIP_MATERIALIZE, DPCLIP_SIMT = 0, 1, 2, 3, 4
 
 _vp, _i, _l, _f = ctypes.c_void_p, ctypes.c_int, ctypes.c_long, ctypes.c_float
@@ -141,10 +142,13 @@ def load_library():
     L.dpclip_qknorm_forward.argtypes = qk + [_vp]
     L.dpclip_qknorm_backward.argtypes = qk + [ctypes.POINTER(_vp), ctypes.POINTER(_vp), _vp, _sz, _vp]
     L.dpclip_qknorm_workspace_bytes.argtypes = [_i] * 5
-    for name in ("dpclip_stored_clipped_grad", "dpclip_relbias_bucket", "dpclip_relbias_forward", "dpclip_relbias_sqnorms",
+    L.dpclip_gated_forward.argtypes = [_vp, _l, _vp, _l, _vp, _i, _i, _i, _i, _i, _vp, _l, _vp, _l, _vp, _sz, _vp]
+    L.dpclip_gated_backward.argtypes = [_vp, _l, _vp, _l, _vp, _l, _i, _i, _i, _i, _i, _vp, _l, _vp, _l, _vp, _sz, _vp]
+    L.dpclip_gated_workspace_bytes.argtypes = [_i] * 4
+    for name in ("dpclip_gated_forward", "dpclip_gated_backward", "dpclip_stored_clipped_grad", "dpclip_relbias_bucket", "dpclip_relbias_forward", "dpclip_relbias_sqnorms",
                  "dpclip_rotation_table", "dpclip_qknorm_forward", "dpclip_qknorm_backward"):
         getattr(L, name).restype = _i
-    for name in ("dpclip_relbias_workspace_bytes", "dpclip_qknorm_workspace_bytes"):
+    for name in ("dpclip_relbias_workspace_bytes", "dpclip_qknorm_workspace_bytes", "dpclip_gated_workspace_bytes"):
         getattr(L, name).restype = _sz
     L.dpclip_workspace_bytes.argtypes = [_i, _i, _i, _i, _i, _i]
     L.dpclip_workspace_bytes.restype = _sz
@@ -990,3 +994,70 @@ def dpclip_qknorm_backward(dq_out: torch.Tensor, dk_out: Optional[torch.Tensor],
                                                _dtype_code(q), grads, sq, workspace.data_ptr(), workspace.nbytes, _stream(stream))
     if rc:
         raise DpclipError("dpclip_qknorm_backward", rc)
+
+
+def _matrix(t: torch.Tensor, dtype, rows: Optional[int], cols: Optional[int]):
+    """A (..., columns) tensor as a matrix of equally spaced rows: (address, row stride, rows, columns)."""
+    if t.dim() == 2:
+        M, n = t.shape
+        ld, inner = t.stride()
+        if M == 1:
+            ld = n
+    else:
+        B, T, n, ld = _rows(t)
+        M, inner = B * T, 1
+    if t.dtype != dtype or (rows is not None and M != rows) or (cols is not None and n != cols) or (inner != 1 and n > 1):
+        raise ValueError(f"expected {dtype} rows ({rows}, {cols}) with contiguous columns, got {t.dtype} {tuple(t.shape)}")
+    return t.data_ptr(), ld, M, n
+
+
+def dpclip_gated_workspace_bytes(M: int, K: int, F: int, dtype: int = DPCLIP_F32) -> int:
+    return load_library().dpclip_gated_workspace_bytes(M, K, F, dtype)
+
+
+def dpclip_gated_forward(X: torch.Tensor, W: torch.Tensor, bias: Optional[torch.Tensor], H: torch.Tensor, Z: Optional[torch.Tensor],
+                         act: int, workspace: torch.Tensor, stream=None) -> None:
+    """H = act(X Wg^T + bg) (.) (X Wu^T + bu).  X (..., K), W (2F, K) gate rows first, bias (2F,) fp32 or None, H (..., F), Z (..., 2F) or
+    None (the pre-activations, for dpclip_gated_backward)."""
+    _on_device(X, W, bias, H, Z, workspace)
+    dt = X.dtype
+    x, ldx, M, K = _matrix(X, dt, None, None)
+    w, ldw, F2, _ = _matrix(W, dt, None, K)
+    F = F2 // 2
+    if F2 % 2:
+        raise ValueError("W must have an even number of rows: gate rows, then up rows")
+    h, ldh, _, _ = _matrix(H, dt, M, F)
+    _writable(H.shape, H.stride())
+    z, ldz = None, 0
+    if Z is not None:
+        z, ldz, _, _ = _matrix(Z, dt, M, F2)
+        _writable(Z.shape, Z.stride())
+    rc = load_library().dpclip_gated_forward(x, ldx, w, ldw, _dense(bias, torch.float32, (F2,)), M, K, F, _dtype_code(X), act, h, ldh, z, ldz,
+                                             workspace.data_ptr(), workspace.nbytes, _stream(stream))
+    if rc:
+        raise DpclipError("dpclip_gated_forward", rc)
+
+
+def dpclip_gated_backward(dH: torch.Tensor, Z: torch.Tensor, W: Optional[torch.Tensor], dZ: torch.Tensor, dX: Optional[torch.Tensor],
+                          act: int, workspace: torch.Tensor, stream=None) -> None:
+    """dZ (..., 2F), the signal of Layer(X, dZ), and dX (..., K) or None, from dH (..., F) and the Z of the forward pass."""
+    _on_device(dH, Z, W, dZ, dX, workspace)
+    dt = Z.dtype
+    z, ldz, M, F2 = _matrix(Z, dt, None, None)
+    F = F2 // 2
+    if F2 % 2:
+        raise ValueError("Z must have an even number of columns: gate, then up")
+    dh, lddh, _, _ = _matrix(dH, dt, M, F)
+    dz, lddz, _, _ = _matrix(dZ, dt, M, F2)
+    _writable(dZ.shape, dZ.stride())
+    w, ldw, K, dx, lddx = None, 0, 1, None, 0
+    if dX is not None:
+        if W is None:
+            raise ValueError("dX needs W")
+        w, ldw, _, K = _matrix(W, dt, F2, None)
+        dx, lddx, _, _ = _matrix(dX, dt, M, K)
+        _writable(dX.shape, dX.stride())
+    rc = load_library().dpclip_gated_backward(dh, lddh, z, ldz, w, ldw, M, K, F, _dtype_code(Z), act, dz, lddz, dx, lddx,
+                                              workspace.data_ptr(), workspace.nbytes, _stream(stream))
+    if rc:
+        raise DpclipError("dpclip_gated_backward", rc)

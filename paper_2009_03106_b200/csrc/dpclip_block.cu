@@ -3,7 +3,10 @@
 #include <stdint.h>
 #include <string.h>
 
+#include <type_traits>
+
 #include "internal.cuh"
+#include "kernels_gated.cuh"
 #include "kernels_qknorm.cuh"
 #include "kernels_relbias.cuh"
 #include "kernels_stored.cuh"
@@ -243,6 +246,145 @@ bool qk_fill(QkParams& p, const dpclip_heads* parts, int n_parts, int B, int T, 
     return vec;
 }
 
+// ------------------------------------------------------------------------------------------------ gated feed-forward block
+constexpr int kPairs = kNumSMs / 2;
+
+// Tile width and split of a product of M rows, `cols` columns (of h, or of dx) and KD contracted, on CTA pairs.  Counted in stages of a
+// 256-column tile (64 of the contraction, 0.28 us): waves of tiles, each as many stages as its part of the contraction and six for filling the
+// pipeline and the last tile's epilogue; a 128-column tile's stage costs 0.6 of it (A is loaded for half the columns); splitting costs a launch
+// and the partial products' way to memory and back.
+struct GatedCut { int hn, splits, kb_per_split; };
+GatedCut gated_cut(long M, long cols, long KD, bool fwd) {
+    const int KB = ceil_div(KD, tc::gt::BK);
+    GatedCut best = {128, 1, KB};
+    double least = 1e30;
+    for (int hn = 64; hn <= 128; hn *= 2)
+        for (int s = 1; s <= 32; s *= 2) {
+            if (s > 1 && KB < 4 * s) break;
+            const long tiles = (long)ceil_div(M, 256) * ceil_div(cols, fwd ? hn : 2 * hn);
+            if (s > 1 && tiles * s > 2 * kPairs) break;
+            const int per = ceil_div(KB, s);
+            double cost = (double)((tiles * s + kPairs - 1) / kPairs) * (per * (hn == 128 ? 1.0 : 0.6) + 6);
+            if (s > 1) cost += 10 + (double)M * cols * (fwd ? 2 : 1) * 4 * (s + 1) / 5e6 / 0.28;
+            if (cost < least) { least = cost; best = {hn, ceil_div(KB, per), per}; }
+        }
+    return best;
+}
+// Split of the same product on the fp32 ALUs: two CTAs an SM, at least 128 contracted each.
+inline int gated_simt_rows(long M) { return M <= 64 ? 32 : 128; }
+inline int gated_simt_splits(long M, long cols, long KD, bool fwd) {
+    const long tiles = (long)ceil_div(M, gated_simt_rows(M)) * ceil_div(cols, fwd ? 64 : 128);
+    return clamp_int(2L * kNumSMs / tiles, 1, clamp_int(KD / 128, 1, 32));
+}
+inline bool gated_rows_ok(const void* p, long ld) { return is_aligned(p, 16) && ld % 8 == 0; }
+inline long up8(long n) { return (n + 7) / 8 * 8; }
+struct GatedSpace { size_t part, copy_a, copy_w; };       // bytes: partial products; copies of an operand of M rows and of W
+GatedSpace gated_space(long M, long K, long F, dpclip_dtype dtype, bool fwd) {
+    const long cols = fwd ? F : K, KD = fwd ? K : 2 * F, width = fwd ? 2 * F : K;
+    const int simt = gated_simt_splits(M, cols, KD, fwd), tensor = dtype == DPCLIP_BF16 ? gated_cut(M, cols, KD, fwd).splits : 1;
+    const int s = simt > tensor ? simt : tensor;
+    GatedSpace g = {s > 1 ? round_up(sizeof(float) * (size_t)s * M * width, 256) : 0, 0, 0};
+    if (dtype == DPCLIP_BF16 && (K % 8 || F % 8)) {
+        g.copy_a = round_up(2 * (size_t)M * up8(KD), 256);
+        g.copy_w = round_up(2 * (size_t)2 * F * up8(K), 256);
+    }
+    return g;
+}
+inline size_t total_bytes(const GatedSpace& g) { return g.part + g.copy_a + g.copy_w; }
+
+int gated_copy(const void* src, long ld, void* dst, long ldd, long rows, long cols, cudaStream_t st) {
+    gated_copy_kernel<<<clamp_int(rows, 1, kNumSMs * 16), 256, 0, st>>>(static_cast<const __nv_bfloat16*>(src), ld, static_cast<__nv_bfloat16*>(dst), ldd, rows, (int)cols);
+    return finish_launch();
+}
+
+template <typename T, bool FWD>
+int launch_gated_reduce(const GatedOut& o, cudaStream_t st) {
+    const long n = (long)o.M * o.F;
+    return launch_after(gated_reduce_kernel<T, FWD>, dim3(clamp_int((n + 255) / 256, 1, kNumSMs * 8)), 256, 0, st, o);
+}
+
+template <typename T, bool FWD>
+int launch_gated_simt(GatedSimt& p, cudaStream_t st) {
+    const int bm = gated_simt_rows(p.M), splits = gated_simt_splits(p.M, p.N, p.KD, FWD);
+    p.tiles_n = ceil_div(p.N, FWD ? 64 : 128);
+    p.k_per_split = (int)round_up(ceil_div(p.KD, splits), 16);
+    p.out.splits = ceil_div(p.KD, p.k_per_split);
+    const long tiles = (long)ceil_div(p.M, bm) * p.tiles_n;
+    if (tiles > 0x7FFFFFFFL) return DPCLIP_ERR_UNSUPPORTED;
+    const dim3 grid((unsigned)tiles, p.out.splits);
+    if (bm == 32) gated_simt_kernel<T, FWD, 32><<<grid, 256, 0, st>>>(p);
+    else gated_simt_kernel<T, FWD, 128><<<grid, 256, 0, st>>>(p);
+    const int rc = finish_launch();
+    return rc || p.out.splits == 1 ? rc : launch_gated_reduce<T, FWD>(p.out, st);
+}
+
+template <typename T, int V, int MT>
+int launch_gated_few(const GatedFew& p, cudaStream_t st) {
+    gated_few_kernel<T, V, MT><<<ceil_div(p.out.F, 4 * GF_ROWS), 128, 0, st>>>(p);
+    return finish_launch();
+}
+template <typename T, int V>
+int launch_gated_few(const GatedFew& p, cudaStream_t st) {
+    const int M = p.out.M;
+    return M == 1 ? launch_gated_few<T, V, 1>(p, st) : M == 2 ? launch_gated_few<T, V, 2>(p, st)
+         : M <= 4 ? launch_gated_few<T, V, 4>(p, st) : launch_gated_few<T, V, 8>(p, st);
+}
+
+template <bool FWD, bool KEEP, int HN>
+int launch_gated_tc(const tc::gt::Maps& maps, const tc::gt::Params& p, cudaStream_t st) {
+    using C = tc::gt::Cfg<FWD, KEEP, HN>;
+    if (cudaFuncSetAttribute(tc::gated_tc_kernel<FWD, KEEP, HN>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM_BYTES) != cudaSuccess)
+        return DPCLIP_ERR_CUDA;
+    const int pairs = p.total < kPairs ? p.total : kPairs;
+    tc::gated_tc_kernel<FWD, KEEP, HN><<<2 * pairs, tc::gt::THREADS, C::SMEM_BYTES, st>>>(maps, p);
+    const int rc = finish_launch();
+    return rc || p.out.splits == 1 ? rc : launch_gated_reduce<__nv_bfloat16, FWD>(p.out, st);
+}
+// a [M][KD] (lda), w [2F][K] (ldw): rows TMA can address
+int gated_tensor(bool fwd, const void* a, long lda, const void* w, long ldw, int M, int K, int F, GatedOut out, int* status, cudaStream_t st) {
+    using namespace tc::gt;
+    const int KD = fwd ? K : 2 * F, cols = fwd ? F : K;
+    const GatedCut cut = gated_cut(M, cols, KD, fwd);
+    Params p;
+    memset(&p, 0, sizeof(p));
+    p.KB = ceil_div(KD, BK);
+    p.kb_per_split = cut.kb_per_split;
+    p.tiles_m = ceil_div(M, 256); p.tiles_n = ceil_div(cols, fwd ? cut.hn : 2 * cut.hn);
+    const long total = (long)p.tiles_m * p.tiles_n * cut.splits;
+    if (total > 0x3FFFFFFFL) return DPCLIP_ERR_UNSUPPORTED;
+    p.total = (int)total;
+    p.status = status; p.out = out; p.out.splits = cut.splits;
+    const bool keep = fwd && out.z && cut.splits == 1;
+    // a store writes whole 16-byte units of a row: rows that end inside one would lose what lies behind them
+    p.tma_out = cols % 8 == 0 && gated_rows_ok(out.h, out.ldh) && (!keep || gated_rows_ok(out.z, out.ldz));
+    Maps maps;
+    memset(&maps, 0, sizeof(maps));
+    const __nv_bfloat16* wb = static_cast<const __nv_bfloat16*>(w);
+    bool ok = encode_map_bf16(&maps.a, a, M, KD, lda, 64, BM_CTA);
+    if (fwd) ok = ok && encode_map_bf16(&maps.b[0], wb, F, K, ldw, 64, cut.hn) && encode_map_bf16(&maps.b[1], wb + (long)F * ldw, F, K, ldw, 64, cut.hn);
+    else ok = ok && encode_map_bf16(&maps.b[0], wb, 2L * F, K, ldw, 64, BK) && encode_map_bf16(&maps.b[1], wb, 2L * F, K, ldw, 64, BK);
+    if (p.tma_out && cut.splits == 1) {
+        ok = ok && encode_map_bf16(&maps.h, out.h, M, cols, out.ldh, 64, 32);
+        if (keep) {
+            __nv_bfloat16* z = static_cast<__nv_bfloat16*>(out.z);
+            ok = ok && encode_map_bf16(&maps.z[0], z, M, F, out.ldz, 64, 32) && encode_map_bf16(&maps.z[1], z + F, M, F, out.ldz, 64, 32);
+        }
+    }
+    if (!ok) return DPCLIP_ERR_CUDA;
+    if (!fwd) return cut.hn == 128 ? launch_gated_tc<false, false, 128>(maps, p, st) : launch_gated_tc<false, false, 64>(maps, p, st);
+    if (keep) return cut.hn == 128 ? launch_gated_tc<true, true, 128>(maps, p, st) : launch_gated_tc<true, true, 64>(maps, p, st);
+    return cut.hn == 128 ? launch_gated_tc<true, false, 128>(maps, p, st) : launch_gated_tc<true, false, 64>(maps, p, st);
+}
+// copies pay from here on: 2 x 2F x K x 2 bytes of copied weights against 4 M F K flops at the fp32 ALUs' rate
+constexpr int kGatedCopyRows = 32;
+
+int gated_check(int M, int K, int F, dpclip_dtype dtype, int act, bool product, const void* workspace, size_t workspace_bytes) {
+    if (M <= 0 || K <= 0 || F <= 0 || F > (1 << 29) || !dtype_known(dtype) || act < DPCLIP_ACT_SILU || act > DPCLIP_ACT_RELU) return DPCLIP_ERR_INVALID_ARG;
+    if (product && (!workspace || !is_aligned(workspace, 256) || workspace_bytes < dpclip_gated_workspace_bytes(M, K, F, dtype)))
+        return DPCLIP_ERR_WORKSPACE;
+    return DPCLIP_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -399,6 +541,98 @@ int dpclip_qknorm_backward(const dpclip_heads* parts, int n_parts, int B, int T,
         any = any || grads[k] || sq_layers[k];
     }
     return any ? launch_after(qknorm_finish_kernel, dim3(B, n_parts), QK_THREADS, 0, st, f) : DPCLIP_OK;
+}
+
+size_t dpclip_gated_workspace_bytes(int M, int K, int F, dpclip_dtype dtype) {
+    if (M <= 0 || K <= 0 || F <= 0 || !dtype_known(dtype)) return kHeaderBytes;
+    const size_t f = total_bytes(gated_space(M, K, F, dtype, true)), b = total_bytes(gated_space(M, K, F, dtype, false));
+    return kHeaderBytes + (f > b ? f : b);
+}
+
+int dpclip_gated_forward(const void* X, long ldx, const void* W, long ldw, const float* bias, int M, int K, int F, dpclip_dtype dtype,
+                         dpclip_activation act, void* H, long ldh, void* Z, long ldz, void* workspace, size_t workspace_bytes, void* stream) {
+    if (!X || !W || !H || ldx < K || ldw < K || ldh < F || (Z && ldz < 2L * F)) return DPCLIP_ERR_INVALID_ARG;
+    int rc = gated_check(M, K, F, dtype, act, true, workspace, workspace_bytes);
+    if (rc) return rc;
+    const size_t es = elt_size(dtype);
+    if (!is_aligned(X, es) || !is_aligned(W, es) || !is_aligned(H, es) || (Z && !is_aligned(Z, es)) || (bias && !is_aligned(bias, 4)))
+        return DPCLIP_ERR_MISALIGNED;
+    cudaStream_t st = (cudaStream_t)stream;
+    const GatedSpace space = gated_space(M, K, F, dtype, true);
+    uint8_t* const ws = static_cast<uint8_t*>(workspace) + kHeaderBytes;
+    GatedOut out;
+    memset(&out, 0, sizeof(out));
+    out.h = H; out.ldh = ldh; out.z = Z; out.ldz = ldz; out.bias = bias; out.M = M; out.F = F; out.act = act; out.splits = 1;
+    out.part = reinterpret_cast<float*>(ws);
+    if (M <= 8) {
+        GatedFew p;
+        memset(&p, 0, sizeof(p));
+        p.x = X; p.ldx = ldx; p.w = W; p.ldw = ldw; p.K = K; p.out = out;
+        const long v = dtype == DPCLIP_F32 ? 4 : 8;
+        const bool vec = is_aligned(X, 16) && is_aligned(W, 16) && ldw % v == 0 && (M == 1 || ldx % v == 0) && K % v == 0;
+        if (dtype == DPCLIP_F32) return vec ? launch_gated_few<float, 4>(p, st) : launch_gated_few<float, 1>(p, st);
+        return vec ? launch_gated_few<__nv_bfloat16, 8>(p, st) : launch_gated_few<__nv_bfloat16, 1>(p, st);
+    }
+    if (dtype == DPCLIP_BF16 && tensor_cores_allowed()) {
+        const bool as_is = gated_rows_ok(X, ldx) && gated_rows_ok(W, ldw);
+        if (as_is || (space.copy_w && M > kGatedCopyRows)) {
+            const void* a = X; const void* w = W;
+            long lda = ldx, ldb = ldw;
+            if (!gated_rows_ok(X, ldx)) { a = ws + space.part; lda = up8(K); rc = gated_copy(X, ldx, ws + space.part, lda, M, K, st); if (rc) return rc; }
+            if (!gated_rows_ok(W, ldw)) { w = ws + space.part + space.copy_a; ldb = up8(K); rc = gated_copy(W, ldw, ws + space.part + space.copy_a, ldb, 2L * F, K, st); if (rc) return rc; }
+            return gated_tensor(true, a, lda, w, ldb, M, K, F, out, static_cast<int*>(workspace), st);
+        }
+    }
+    GatedSimt p;
+    memset(&p, 0, sizeof(p));
+    p.a = X; p.lda = ldx; p.w = W; p.ldw = ldw; p.M = M; p.N = F; p.KD = K; p.out = out;
+    return dtype == DPCLIP_F32 ? launch_gated_simt<float, true>(p, st) : launch_gated_simt<__nv_bfloat16, true>(p, st);
+}
+
+int dpclip_gated_backward(const void* dH, long lddh, const void* Z, long ldz, const void* W, long ldw, int M, int K, int F,
+                          dpclip_dtype dtype, dpclip_activation act, void* dZ, long lddz, void* dX, long lddx,
+                          void* workspace, size_t workspace_bytes, void* stream) {
+    if (!dH || !Z || !dZ || lddh < F || ldz < 2L * F || lddz < 2L * F || (dX && (!W || ldw < K || lddx < K))) return DPCLIP_ERR_INVALID_ARG;
+    int rc = gated_check(M, K, F, dtype, act, dX != nullptr, workspace, workspace_bytes);
+    if (rc) return rc;
+    const size_t es = elt_size(dtype);
+    if (!is_aligned(dH, es) || !is_aligned(Z, es) || !is_aligned(dZ, es) || (dX && (!is_aligned(dX, es) || !is_aligned(W, es)))) return DPCLIP_ERR_MISALIGNED;
+    cudaStream_t st = (cudaStream_t)stream;
+    const GatedSpace space = gated_space(M, K, F, dtype, false);
+    uint8_t* const ws = static_cast<uint8_t*>(workspace) + kHeaderBytes;
+    const bool dz_ok = gated_rows_ok(dZ, lddz), w_ok = dX && gated_rows_ok(W, ldw);
+    const bool tensor = dX && dtype == DPCLIP_BF16 && tensor_cores_allowed() && ((dz_ok && w_ok) || (space.copy_w && M > kGatedCopyRows));
+    GatedSignal s;
+    memset(&s, 0, sizeof(s));
+    s.dh = dH; s.lddh = lddh; s.z = Z; s.ldz = ldz; s.dz = dZ; s.lddz = lddz; s.M = M; s.F = F; s.act = act;
+    if (tensor && !dz_ok) { s.copy = ws + space.part; s.ldc = up8(2L * F); }
+    const long v = dtype == DPCLIP_F32 ? 4 : 8;
+    const bool vec = is_aligned(dH, 16) && is_aligned(Z, 16) && is_aligned(dZ, 16) && F % v == 0 && lddh % v == 0 && ldz % v == 0 && lddz % v == 0;
+    const int grid = clamp_int(M, 1, kNumSMs * 8);
+    if (dtype == DPCLIP_F32) {
+        if (vec) gated_signal_kernel<float, 4><<<grid, 256, 0, st>>>(s);
+        else gated_signal_kernel<float, 1><<<grid, 256, 0, st>>>(s);
+    } else {
+        if (vec) gated_signal_kernel<__nv_bfloat16, 8><<<grid, 256, 0, st>>>(s);
+        else gated_signal_kernel<__nv_bfloat16, 1><<<grid, 256, 0, st>>>(s);
+    }
+    rc = finish_launch();
+    if (rc || !dX) return rc;
+    GatedOut out;
+    memset(&out, 0, sizeof(out));
+    out.h = dX; out.ldh = lddx; out.M = M; out.F = K; out.splits = 1;
+    out.part = reinterpret_cast<float*>(ws);
+    if (tensor) {
+        const void* a = dz_ok ? dZ : s.copy;
+        const void* w = W;
+        long ldb = ldw;
+        if (!w_ok) { w = ws + space.part + space.copy_a; ldb = up8(K); rc = gated_copy(W, ldw, ws + space.part + space.copy_a, ldb, 2L * F, K, st); if (rc) return rc; }
+        return gated_tensor(false, a, dz_ok ? lddz : s.ldc, w, ldb, M, K, F, out, static_cast<int*>(workspace), st);
+    }
+    GatedSimt p;
+    memset(&p, 0, sizeof(p));
+    p.a = dZ; p.lda = lddz; p.w = W; p.ldw = ldw; p.M = M; p.N = K; p.KD = 2 * F; p.out = out;
+    return dtype == DPCLIP_F32 ? launch_gated_simt<float, false>(p, st) : launch_gated_simt<__nv_bfloat16, false>(p, st);
 }
 
 }  // extern "C"

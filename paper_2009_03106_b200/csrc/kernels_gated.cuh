@@ -1,0 +1,611 @@
+// Gated feed-forward block: zg = X Wg^T + bg, zu = X Wu^T + bu, h = act(zg) (.) zu, with the weight [2F][K] of both projections (gate
+// rows, then up rows); backward: dzg = dh (.) zu (.) act'(zg), dzu = dh (.) act(zg), dx = [dzg dzu] W.
+//
+//   gated_tc_kernel      bf16 products on CTA pairs (tcgen05, cta_group::2).  Forward: a pair's tile is 256 rows by HN gate and the HN
+//                        up columns that go with them -- CTA 0 loads the gate rows of W, CTA 1 the up rows, and the accumulator of both
+//                        lies side by side in each CTA's tensor memory, so that activation and product are the epilogue.  Backward: the
+//                        plain product dZ W, with W read as it lies (its contraction index is the row: MN-major operand).
+//   gated_simt_kernel    the same two products on the fp32 ALUs: fp32 inputs, and rows that TMA cannot address.
+//   gated_few_kernel     up to eight rows of X: the weights are streamed once, a warp takes two gate and two up rows.
+//   gated_reduce_kernel  adds up the partial products of a split contraction, in order, and ends as the products' epilogue does.
+//   gated_signal_kernel  dh, z -> dz: five passes over M x F numbers, bound by memory.
+//
+// Pre-activations and products are fp32; h, z, dz and dx are rounded once.  The backward pass starts from the stored z and multiplies W with
+// the stored dz, so in bf16 both carry that type's rounding.
+#pragma once
+#include "internal.cuh"
+#include "tc_common.cuh"
+
+namespace dpclip {
+
+// ------------------------------------------------------------------------------------------------ activations
+// EXACT: expf and a correctly rounded division, for fp32 results; else the fast forms (a few 2^-21), for bf16 ones.
+template <bool EXACT> __device__ __forceinline__ float gate_sigmoid(float z) {
+    return EXACT ? 1.f / (1.f + expf(-z)) : __fdividef(1.f, 1.f + __expf(-z));
+}
+constexpr float kGeluTanh = 0.7978845608028654f, kGeluCube = 0.044715f;       // sqrt(2 / pi)
+
+template <int ACT, bool EXACT> __device__ __forceinline__ float gate_act(float z) {
+    if constexpr (ACT == DPCLIP_ACT_SILU) return z * gate_sigmoid<EXACT>(z);
+    else if constexpr (ACT == DPCLIP_ACT_RELU) return z < 0.f ? 0.f : z;
+    else if constexpr (ACT == DPCLIP_ACT_GELU) return 0.5f * z * (1.f + erff(z * 0.70710678118654752f));
+    else return z * gate_sigmoid<EXACT>(2.f * kGeluTanh * z * fmaf(kGeluCube * z, z, 1.f));     // (1 + tanh u) / 2 = sigmoid(2 u)
+}
+// the activation and its derivative
+template <int ACT, bool EXACT> __device__ __forceinline__ void gate_act_grad(float z, float& a, float& da) {
+    if constexpr (ACT == DPCLIP_ACT_SILU) {
+        const float p = gate_sigmoid<EXACT>(z);
+        a = z * p;
+        da = p * fmaf(z, 1.f - p, 1.f);
+    } else if constexpr (ACT == DPCLIP_ACT_RELU) {
+        a = z < 0.f ? 0.f : z;
+        da = z > 0.f ? 1.f : 0.f;
+    } else if constexpr (ACT == DPCLIP_ACT_GELU) {
+        const float c = 0.5f * (1.f + erff(z * 0.70710678118654752f));
+        a = z * c;
+        const float e = EXACT ? expf(-0.5f * z * z) : __expf(-0.5f * z * z);
+        da = fmaf(z * 0.3989422804014327f, e, c);                              // 1 / sqrt(2 pi)
+    } else {
+        const float p = gate_sigmoid<EXACT>(2.f * kGeluTanh * z * fmaf(kGeluCube * z, z, 1.f));
+        a = z * p;
+        da = fmaf(a * (1.f - p), 2.f * kGeluTanh * fmaf(3.f * kGeluCube * z, z, 1.f), p);
+    }
+}
+template <bool EXACT, typename F> __device__ __forceinline__ void gate_dispatch(int act, F f) {
+    switch (act) {
+        case DPCLIP_ACT_SILU: f(std::integral_constant<int, DPCLIP_ACT_SILU>()); break;
+        case DPCLIP_ACT_GELU: f(std::integral_constant<int, DPCLIP_ACT_GELU>()); break;
+        case DPCLIP_ACT_GELU_TANH: f(std::integral_constant<int, DPCLIP_ACT_GELU_TANH>()); break;
+        default: f(std::integral_constant<int, DPCLIP_ACT_RELU>()); break;
+    }
+}
+__device__ __forceinline__ void gate_store(float* p, float v) { *p = v; }
+__device__ __forceinline__ void gate_store(__nv_bfloat16* p, float v) { *p = __float2bfloat16_rn(v); }
+
+// ------------------------------------------------------------------------------------------------ dz from dh and z
+struct GatedSignal {
+    const void* dh; long lddh;
+    const void* z; long ldz;             // [M][2F]
+    void* dz; long lddz;                 // [M][2F], may be z
+    void* copy; long ldc;                // NULL, or a second place for dz with 16-byte rows
+    long M; int F, act;
+};
+template <typename T, int V>             // V elements a thread: 16 bytes, or one
+__global__ void __launch_bounds__(256)
+gated_signal_kernel(const __grid_constant__ GatedSignal p) {
+    constexpr bool EXACT = sizeof(T) == 4;
+    const int per_row = (p.F + V - 1) / V;
+    const uint32_t row_step = gridDim.x;
+    gate_dispatch<EXACT>(p.act, [&](auto a) {
+        constexpr int ACT = decltype(a)::value;
+        for (long m = blockIdx.x; m < p.M; m += row_step) {
+            const T* const dh = static_cast<const T*>(p.dh) + m * p.lddh;
+            const T* const zg = static_cast<const T*>(p.z) + m * p.ldz;
+            T* const og = static_cast<T*>(p.dz) + m * p.lddz;
+            T* const oc = p.copy ? static_cast<T*>(p.copy) + m * p.ldc : nullptr;
+            auto one = [&](float h, float g, float u, float& dg, float& du) {
+                float act, slope;
+                gate_act_grad<ACT, EXACT>(g, act, slope);
+                dg = h * u * slope;
+                du = h * act;
+            };
+            if constexpr (V == 1) {
+#pragma unroll 4
+                for (int f = threadIdx.x; f < per_row; f += 256) {
+                    float dg, du;
+                    one(to_f32(dh[f]), to_f32(zg[f]), to_f32(zg[p.F + f]), dg, du);
+                    gate_store(og + f, dg); gate_store(og + p.F + f, du);
+                    if (oc) { gate_store(oc + f, dg); gate_store(oc + p.F + f, du); }
+                }
+            } else {
+#pragma unroll 2
+                for (int c = threadIdx.x; c < per_row; c += 256) {
+                    const int f = c * V;
+                    const uint4 h = *reinterpret_cast<const uint4*>(dh + f), g = *reinterpret_cast<const uint4*>(zg + f),
+                                u = *reinterpret_cast<const uint4*>(zg + p.F + f);
+                    const uint32_t hw[4] = {h.x, h.y, h.z, h.w}, gw[4] = {g.x, g.y, g.z, g.w}, uw[4] = {u.x, u.y, u.z, u.w};
+                    uint32_t a[4], b[4];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        float x0, x1, y0, y1;
+                        if constexpr (V == 8) {
+                            one(__uint_as_float(hw[k] << 16), __uint_as_float(gw[k] << 16), __uint_as_float(uw[k] << 16), x0, y0);
+                            one(__uint_as_float(hw[k] & 0xFFFF0000u), __uint_as_float(gw[k] & 0xFFFF0000u), __uint_as_float(uw[k] & 0xFFFF0000u), x1, y1);
+                            a[k] = f32x2_to_bf16x2(make_f32x2(x0, x1));
+                            b[k] = f32x2_to_bf16x2(make_f32x2(y0, y1));
+                        } else {
+                            one(__uint_as_float(hw[k]), __uint_as_float(gw[k]), __uint_as_float(uw[k]), x0, y0);
+                            a[k] = __float_as_uint(x0); b[k] = __float_as_uint(y0);
+                        }
+                    }
+                    *reinterpret_cast<uint4*>(og + f) = make_uint4(a[0], a[1], a[2], a[3]);
+                    *reinterpret_cast<uint4*>(og + p.F + f) = make_uint4(b[0], b[1], b[2], b[3]);
+                }
+            }
+        }
+    });
+}
+
+// rows of any stride and start copied to rows of 16-byte multiples
+__global__ void __launch_bounds__(256)
+gated_copy_kernel(const __nv_bfloat16* __restrict__ src, long ld, __nv_bfloat16* __restrict__ dst, long ldd, long rows, int cols) {
+    for (long m = blockIdx.x; m < rows; m += gridDim.x) {
+#pragma unroll 4
+        for (int c = threadIdx.x; c < cols; c += 256) dst[m * ldd + c] = src[m * ld + c];
+    }
+}
+
+// ------------------------------------------------------------------------------------------------ products: what they share
+struct GatedOut {
+    void* h; long ldh;                   // forward: h [M][F];  backward: dx [M][N]
+    void* z; long ldz;                   // forward: [M][2F] or NULL
+    const float* bias;                   // forward: [2F] or NULL
+    int M, F, act;                       // F: columns of h, or of dx
+    float* part; int splits;             // splits > 1: partial products [splits][M][2F] (forward) or [splits][M][F]
+};
+template <typename T> __device__ __forceinline__ void gated_end(const GatedOut& o, long m, int f, float g, float u) {
+    constexpr bool EXACT = sizeof(T) == 4;
+    if (o.bias) { g += __ldg(o.bias + f); u += __ldg(o.bias + o.F + f); }
+    float h = 0.f;
+    gate_dispatch<EXACT>(o.act, [&](auto a) { h = gate_act<decltype(a)::value, EXACT>(g) * u; });
+    gate_store(static_cast<T*>(o.h) + m * o.ldh + f, h);
+    if (o.z) { gate_store(static_cast<T*>(o.z) + m * o.ldz + f, g); gate_store(static_cast<T*>(o.z) + m * o.ldz + o.F + f, u); }
+}
+template <typename T, bool FWD>
+__global__ void __launch_bounds__(256)
+gated_reduce_kernel(const __grid_constant__ GatedOut o) {
+    griddep_wait();
+    const long n = (long)o.M * o.F, width = FWD ? 2L * o.F : o.F, plane = (long)o.M * width;
+    for (long i = (long)blockIdx.x * 256 + threadIdx.x; i < n; i += (long)gridDim.x * 256) {
+        const long m = i / o.F;
+        const int f = (int)(i - m * o.F);
+        const float* src = o.part + m * width + f;
+        float g = 0.f, u = 0.f;
+#pragma unroll 4
+        for (int s = 0; s < o.splits; ++s) { g += src[s * plane]; if (FWD) u += src[s * plane + o.F]; }
+        if (FWD) gated_end<T>(o, m, f, g, u);
+        else gate_store(static_cast<T*>(o.h) + m * o.ldh + f, g);
+    }
+}
+
+// ------------------------------------------------------------------------------------------------ fp32 ALUs
+// 256 threads, BM x 128 tile of the product (forward: 64 gate and 64 up columns, so a thread holds both of a column), 16 of the contraction a
+// step, the next step's operands in registers while this one's are multiplied from shared memory.
+struct GatedSimt {
+    const void* a; long lda;             // X [M][K] or dZ [M][2F]
+    const void* w; long ldw;             // [2F][K]
+    int M, N, KD;                        // N: columns of h or dx; KD: the contraction
+    int tiles_n, k_per_split;            // k_per_split: a multiple of 16
+    GatedOut out;
+};
+template <typename T, bool FWD, int BM>
+__global__ void __launch_bounds__(256)
+gated_simt_kernel(const __grid_constant__ GatedSimt p) {
+    constexpr int BN = 128, BK = 16, RM = BM / 16, LA = BM * BK / 256, LB = BN * BK / 256, HALF = FWD ? 64 : 128;
+    __shared__ __align__(16) float as[2][BK][BM + 4], bs[2][BK][BN + 4];
+    const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
+    const int tm = blockIdx.x / p.tiles_n, tn = blockIdx.x - tm * p.tiles_n;
+    const int m0 = tm * BM, n0 = tn * HALF;
+    const int k_begin = blockIdx.y * p.k_per_split, k_end = min(p.KD, k_begin + p.k_per_split);
+    const T* const a = static_cast<const T*>(p.a);
+    const T* const w = static_cast<const T*>(p.w);
+    float ra[LA], rb[LB];
+    auto fetch = [&](int k0) {
+#pragma unroll
+        for (int i = 0; i < LA; ++i) {
+            const int k = k0 + tx, m = m0 + ty + 16 * i;
+            ra[i] = k < k_end && m < p.M ? to_f32(a[(long)m * p.lda + k]) : 0.f;
+        }
+#pragma unroll
+        for (int i = 0; i < LB; ++i) {
+            if constexpr (FWD) {
+                const int k = k0 + tx, j = ty + 16 * i, f = n0 + (j & 63);
+                rb[i] = k < k_end && f < p.N ? to_f32(w[(long)(f + (j >= 64 ? p.N : 0)) * p.ldw + k]) : 0.f;
+            } else {
+                const int k = k0 + (tid >> 7) + 2 * i, n = n0 + (tid & 127);
+                rb[i] = k < k_end && n < p.N ? to_f32(w[(long)k * p.ldw + n]) : 0.f;
+            }
+        }
+    };
+    auto put = [&](int b) {
+#pragma unroll
+        for (int i = 0; i < LA; ++i) as[b][tx][ty + 16 * i] = ra[i];
+#pragma unroll
+        for (int i = 0; i < LB; ++i) {
+            if constexpr (FWD) bs[b][tx][ty + 16 * i] = rb[i];
+            else bs[b][(tid >> 7) + 2 * i][tid & 127] = rb[i];
+        }
+    };
+    // thread's rows: ty * 4 + r and 64 + ty * 4 + r (BM = 128), or ty * 2 + r (BM = 32); columns: tx * 4 + c and 64 + tx * 4 + c
+    float acc[RM][8];
+#pragma unroll
+    for (int r = 0; r < RM; ++r)
+#pragma unroll
+        for (int c = 0; c < 8; ++c) acc[r][c] = 0.f;
+    fetch(k_begin);
+    put(0);
+    __syncthreads();
+    int buf = 0;
+    for (int k0 = k_begin; k0 < k_end; k0 += BK) {
+        const bool more = k0 + BK < k_end;
+        if (more) fetch(k0 + BK);
+#pragma unroll
+        for (int k = 0; k < BK; ++k) {
+            float x[RM], y[8];
+            if constexpr (RM == 8) {
+                const float4 u = *reinterpret_cast<const float4*>(&as[buf][k][ty * 4]), v = *reinterpret_cast<const float4*>(&as[buf][k][64 + ty * 4]);
+                x[0] = u.x; x[1] = u.y; x[2] = u.z; x[3] = u.w; x[4] = v.x; x[5] = v.y; x[6] = v.z; x[7] = v.w;
+            } else {
+                const float2 u = *reinterpret_cast<const float2*>(&as[buf][k][ty * 2]);
+                x[0] = u.x; x[1] = u.y;
+            }
+            const float4 u = *reinterpret_cast<const float4*>(&bs[buf][k][tx * 4]), v = *reinterpret_cast<const float4*>(&bs[buf][k][64 + tx * 4]);
+            y[0] = u.x; y[1] = u.y; y[2] = u.z; y[3] = u.w; y[4] = v.x; y[5] = v.y; y[6] = v.z; y[7] = v.w;
+#pragma unroll
+            for (int r = 0; r < RM; ++r)
+#pragma unroll
+                for (int c = 0; c < 8; ++c) acc[r][c] = fmaf(x[r], y[c], acc[r][c]);
+        }
+        if (more) put(buf ^ 1);
+        buf ^= 1;
+        __syncthreads();
+    }
+#pragma unroll
+    for (int r = 0; r < RM; ++r) {
+        const int m = m0 + (RM == 8 ? (r >> 2) * 64 + ty * 4 + (r & 3) : ty * 2 + r);
+        if (m >= p.M) continue;
+        if constexpr (FWD) {
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                const int f = n0 + tx * 4 + c;
+                if (f >= p.N) continue;
+                if (p.out.splits > 1) {
+                    float* to = p.out.part + ((long)blockIdx.y * p.M + m) * 2 * p.N + f;
+                    to[0] = acc[r][c]; to[p.N] = acc[r][c + 4];
+                } else {
+                    gated_end<T>(p.out, m, f, acc[r][c], acc[r][c + 4]);
+                }
+            }
+        } else {
+#pragma unroll
+            for (int c = 0; c < 8; ++c) {
+                const int n = n0 + (c >> 2) * 64 + tx * 4 + (c & 3);
+                if (n >= p.N) continue;
+                if (p.out.splits > 1) p.out.part[((long)blockIdx.y * p.M + m) * p.N + n] = acc[r][c];
+                else gate_store(static_cast<T*>(p.out.h) + (long)m * p.out.ldh + n, acc[r][c]);
+            }
+        }
+    }
+}
+
+// ------------------------------------------------------------------------------------------------ a few rows of X
+struct GatedFew {
+    const void* x; long ldx;
+    const void* w; long ldw;
+    int K;
+    GatedOut out;
+};
+template <typename T, int V> __device__ __forceinline__ void gated_vec(const T* p, float (&x)[V]) {
+    if constexpr (V == 1) x[0] = to_f32(*p);
+    else if constexpr (V == 4) {
+        const float4 v = __ldg(reinterpret_cast<const float4*>(p));
+        x[0] = v.x; x[1] = v.y; x[2] = v.z; x[3] = v.w;
+    } else {
+        const uint4 v = __ldg(reinterpret_cast<const uint4*>(p));
+        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) { x[2 * k] = __uint_as_float(w[k] << 16); x[2 * k + 1] = __uint_as_float(w[k] & 0xFFFF0000u); }
+    }
+}
+constexpr int GF_ROWS = 2;               // gate rows of W a warp, and as many up rows
+template <typename T, int V, int MT>
+__global__ void __launch_bounds__(128)
+gated_few_kernel(const __grid_constant__ GatedFew p) {
+    const int lane = threadIdx.x & 31, f0 = (blockIdx.x * 4 + (threadIdx.x >> 5)) * GF_ROWS;
+    const int F = p.out.F, M = p.out.M;
+    if (f0 >= F) return;
+    const T* row[2 * GF_ROWS];
+#pragma unroll
+    for (int r = 0; r < GF_ROWS; ++r) {
+        const int f = min(f0 + r, F - 1);
+        row[r] = static_cast<const T*>(p.w) + (long)f * p.ldw;
+        row[GF_ROWS + r] = static_cast<const T*>(p.w) + (long)(F + f) * p.ldw;
+    }
+    float acc[2 * GF_ROWS][MT];
+#pragma unroll
+    for (int r = 0; r < 2 * GF_ROWS; ++r)
+#pragma unroll
+        for (int m = 0; m < MT; ++m) acc[r][m] = 0.f;
+#pragma unroll 2
+    for (int k = lane * V; k < p.K; k += 32 * V) {
+        float w[2 * GF_ROWS][V];
+#pragma unroll
+        for (int r = 0; r < 2 * GF_ROWS; ++r) gated_vec<T, V>(row[r] + k, w[r]);
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
+            if (m < M) {
+                float x[V];
+                gated_vec<T, V>(static_cast<const T*>(p.x) + (long)m * p.ldx + k, x);
+#pragma unroll
+                for (int r = 0; r < 2 * GF_ROWS; ++r)
+#pragma unroll
+                    for (int v = 0; v < V; ++v) acc[r][m] = fmaf(w[r][v], x[v], acc[r][m]);
+            }
+        }
+    }
+#pragma unroll
+    for (int r = 0; r < 2 * GF_ROWS; ++r)
+#pragma unroll
+        for (int m = 0; m < MT; ++m) acc[r][m] = warp_sum(acc[r][m]);
+    // lane (m, r) writes; a choice among registers, not an index into them
+    float g = 0.f, u = 0.f;
+#pragma unroll
+    for (int r = 0; r < GF_ROWS; ++r)
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+            if (lane == m * GF_ROWS + r) { g = acc[r][m]; u = acc[GF_ROWS + r][m]; }
+    const int m = lane / GF_ROWS, f = f0 + lane % GF_ROWS;
+    if (m < M && m < MT && f < F) gated_end<T>(p.out, m, f, g, u);
+}
+
+// ------------------------------------------------------------------------------------------------ tensor cores
+namespace tc {
+namespace gt {
+constexpr int BK = 64, BM_CTA = 128;
+constexpr int A_BYTES = BM_CTA * 128;                    // 128 rows x 64 bf16
+constexpr int EPI_WARPS = 8, THREADS = 64 + 32 * EPI_WARPS;
+constexpr int BOX_BYTES = 32 * 128;                      // 32 rows x 64 bf16 of an output
+// boxes of outputs a warp stages: forward h (and zg, zu) of its 32 rows x 64 columns; backward 32 rows x 2 HN / 2 columns
+template <bool FWD, bool KEEP, int HN> struct Cfg {
+    static constexpr int BOXES = FWD ? (KEEP ? 3 : 1) : HN / 64;
+    static constexpr int STAGE_BYTES = A_BYTES + HN * 128;
+    static constexpr int STAGING = EPI_WARPS * BOXES * BOX_BYTES;
+    static constexpr int STAGES = (224 * 1024 - STAGING) / STAGE_BYTES;
+    static constexpr int SMEM_BYTES = STAGES * STAGE_BYTES + STAGING + 256 + 1024;
+};
+struct Maps { CUtensorMap a, b[2], h, z[2]; };           // b: rows of CTA 0 and of CTA 1; h: output (dx); z: gate and up halves of Z
+struct Params {
+    int KB;                              // stages of the contraction
+    int kb_per_split;
+    int tiles_m, tiles_n, total;         // total: with splits
+    int tma_out;                         // outputs go by TMA; else by plain stores
+    int* status;
+    GatedOut out;
+};
+// Tiles in groups of eight rows of tiles, along the rows first: 74 pairs then work on an 8 x 9 block of the product, whose operands stay in L2.
+struct Tile { int m, n, split; };
+__device__ __forceinline__ Tile tile_at(const Params& p, int t) {
+    Tile w;
+    const int tiles = p.tiles_m * p.tiles_n;
+    w.split = t / tiles;
+    t -= w.split * tiles;
+    const int group = t / (8 * p.tiles_n), rows = min(8, p.tiles_m - group * 8);
+    t -= group * 8 * p.tiles_n;
+    w.n = t / rows;
+    w.m = group * 8 + t - w.n * rows;
+    return w;
+}
+__device__ __forceinline__ void tma_load_2d_pair(void* smem_dst, const CUtensorMap* map, uint32_t bar, int x, int y) {
+    // the bytes are counted on a barrier of CTA 0 of the pair, whichever of the two loads
+    asm volatile(
+        "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
+        ::"r"(smem_u32(smem_dst)), "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(x), "r"(y)
+        : "memory");
+}
+__device__ __forceinline__ void tma_store_2d(const CUtensorMap* map, const void* smem_src, int x, int y) {
+    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%2, %3}], [%1];"
+                 ::"l"(reinterpret_cast<uint64_t>(map)), "r"(smem_u32(smem_src)), "r"(x), "r"(y) : "memory");
+}
+__device__ __forceinline__ void bulk_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
+__device__ __forceinline__ void bulk_wait_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
+__device__ __forceinline__ void bulk_wait() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
+}  // namespace gt
+
+// Warp 0: loads of this CTA's operands (A rows; gate or up rows of W, or half of the columns of W), all counted on CTA 0's `full`; warp 1 of
+// CTA 0: MMAs, commits to both CTAs' `empty` and `acc_full`; eight epilogue warps a CTA: two for each quarter of the tensor-memory lanes.
+// The accumulator is double-buffered (2 x 2 HN <= 512 columns), so a tile's epilogue runs under the next tile's MMAs.  Every wait is bounded.
+template <bool FWD, bool KEEP, int HN>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(gt::THREADS, 1)
+gated_tc_kernel(const __grid_constant__ gt::Maps maps, const __grid_constant__ gt::Params p) {
+    using namespace gt;
+    using C = Cfg<FWD, KEEP, HN>;
+    constexpr int STAGES = C::STAGES, STAGE_BYTES = C::STAGE_BYTES, N = 2 * HN;
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);     // the same offset in both CTAs
+    uint8_t* staging = smem + STAGES * STAGE_BYTES;
+    uint64_t* full = reinterpret_cast<uint64_t*>(staging + C::STAGING);              // CTA 0's are used
+    uint64_t* empty = full + STAGES;                                                 // each CTA's own
+    uint64_t* acc_full = empty + STAGES;                                             // [2], each CTA's own
+    uint64_t* acc_empty = acc_full + 2;                                              // [2], CTA 0's are used
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(acc_empty + 2);
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = cluster_ctarank();
+    const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < STAGES; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], 1); }
+        for (int b = 0; b < 2; ++b) { mbar_init(&acc_full[b], 1); mbar_init(&acc_empty[b], 2 * EPI_WARPS); }
+        *abort_flag = 0;
+        mbar_fence_init();
+        tma_prefetch_desc(&maps.a); tma_prefetch_desc(&maps.b[rank]);
+    }
+    if (warp == 1) { tmem_alloc_pair(tmem_slot, 512); tmem_relinquish_pair(); }
+    tc_fence_before_sync();
+    cluster_sync_all();
+    tc_fence_after_sync();
+    const uint32_t tmem_base = *tmem_slot;
+    griddep_wait();                      // operands that a launch in front of this one has laid out
+
+    if (warp == 0) {
+        if (lane == 0) {
+            const uint32_t full0 = mapa_shared(smem_u32(full), 0);
+            int stage = 0; uint32_t phase = 0;
+            bool ok = true;
+            for (int t = pair; t < p.total && ok; t += pairs) {
+                const Tile w = tile_at(p, t);
+                const int kb0 = w.split * p.kb_per_split, kb1 = min(p.KB, kb0 + p.kb_per_split);
+                const int m0 = w.m * 2 * BM_CTA + (int)rank * BM_CTA;
+                for (int kb = kb0; kb < kb1; ++kb) {
+                    ok = mbar_wait(&empty[stage], phase ^ 1, abort_flag, p.status);
+                    if (!ok) break;
+                    uint8_t* dst = smem + stage * STAGE_BYTES;
+                    const uint32_t bar = full0 + stage * 8;
+                    if (rank == 0) mbar_arrive_expect_tx(&full[stage], 2 * STAGE_BYTES);
+                    tma_load_2d_pair(dst, &maps.a, bar, kb * BK, m0);
+                    if constexpr (FWD) {
+                        tma_load_2d_pair(dst + A_BYTES, &maps.b[rank], bar, kb * BK, w.n * HN);
+                    } else {
+#pragma unroll
+                        for (int c = 0; c < HN / 64; ++c)
+                            tma_load_2d_pair(dst + A_BYTES + c * 8192, &maps.b[rank], bar, w.n * N + (int)rank * HN + c * 64, kb * BK);
+                    }
+                    if (++stage == STAGES) { stage = 0; phase ^= 1; }
+                }
+            }
+        }
+    } else if (warp == 1) {
+        if (lane == 0 && rank == 0) {
+            constexpr uint32_t idesc = make_idesc_bf16(256, N, 0, FWD ? 0 : 1);
+            int stage = 0, it = 0; uint32_t phase = 0;
+            bool ok = true;
+            for (int t = pair; t < p.total && ok; t += pairs, ++it) {
+                const Tile w = tile_at(p, t);
+                const int kb0 = w.split * p.kb_per_split, kb1 = min(p.KB, kb0 + p.kb_per_split);
+                const int buf = it & 1;
+                ok = mbar_wait(&acc_empty[buf], ((it >> 1) & 1) ^ 1, abort_flag, p.status);
+                if (!ok) break;
+                tc_fence_after_sync();
+                for (int kb = kb0; kb < kb1; ++kb) {
+                    ok = mbar_wait(&full[stage], phase, abort_flag, p.status);
+                    if (!ok) break;
+                    tc_fence_after_sync();
+                    const uint32_t a = smem_u32(smem + stage * STAGE_BYTES), b = a + A_BYTES;
+#pragma unroll
+                    for (int k4 = 0; k4 < BK / 16; ++k4) {
+                        const uint64_t da = make_smem_desc_sw128(a + k4 * 32, 16, 1024);
+                        const uint64_t db = FWD ? make_smem_desc_sw128(b + k4 * 32, 16, 1024) : make_smem_desc_sw128(b + k4 * 2048, 8192, 1024);
+                        mma_bf16_ss_pair(tmem_base + buf * N, da, db, idesc, (kb == kb0 && k4 == 0) ? 0u : 1u);
+                    }
+                    mma_commit_pair(&empty[stage], 3);
+                    if (++stage == STAGES) { stage = 0; phase ^= 1; }
+                }
+                if (!ok) break;
+                mma_commit_pair(&acc_full[buf], 3);
+            }
+        }
+    } else {
+        const int quarter = warp & 3, half = (warp - 2) >> 2;
+        uint8_t* const boxes = staging + (warp - 2) * C::BOXES * BOX_BYTES;
+        const uint32_t acc_empty0 = mapa_shared(smem_u32(acc_empty), 0);
+        const GatedOut& o = p.out;
+        // forward: a warp has 64 columns of h (the second half of the warps only when HN = 128); backward: HN columns of dx
+        constexpr int CHUNKS = FWD ? 2 : HN / 32;
+        const bool mine = !FWD || HN == 128 || half == 0;
+        const int c0 = FWD ? half * 64 : half * HN;                          // first column within the tile
+        int it = 0;
+        for (int t = pair; t < p.total; t += pairs, ++it) {
+            const Tile w = tile_at(p, t);
+            const int buf = it & 1;
+            const int row0 = w.m * 2 * BM_CTA + (int)rank * BM_CTA + quarter * 32;
+            const int col0 = w.n * (FWD ? HN : N) + c0;
+            if (!mbar_wait(&acc_full[buf], (it >> 1) & 1, abort_flag, p.status)) break;
+            tc_fence_after_sync();
+            const uint32_t tm = tmem_base + ((uint32_t)(quarter * 32) << 16) + buf * N + c0;
+            const bool there = mine && row0 < o.M && col0 < o.F;
+            if (there && o.splits == 1) { if (lane == 0) bulk_wait_read(); __syncwarp(); }
+#pragma unroll 1
+            for (int c = 0; c < CHUNKS; ++c) {
+                if (!there) break;
+                uint32_t g[32], u[32];
+                tmem_ld_32x32(tm + c * 32, g);
+                if (FWD) tmem_ld_32x32(tm + HN + c * 32, u);
+                tmem_ld_wait();
+                const int col = col0 + c * 32;
+                if (o.splits > 1) {
+                    // partial products: a thread's row, 128 bytes of it
+                    const int m = row0 + lane;
+                    if (m < o.M) {
+                        float* to = o.part + ((long)w.split * o.M + m) * (FWD ? 2L * o.F : o.F) + col;
+#pragma unroll
+                        for (int j = 0; j < 32; ++j)
+                            if (col + j < o.F) { to[j] = __uint_as_float(g[j]); if (FWD) to[o.F + j] = __uint_as_float(u[j]); }
+                    }
+                    continue;
+                }
+                // 32 columns of a row = four 16-byte slots of a 128-byte row, at their swizzled places
+                uint8_t* const box = boxes + (FWD ? 0 : (c >> 1) * BOX_BYTES) + lane * 128;
+                const int slot = (c & 1) * 4, sw = lane & 7;
+                auto put = [&](uint8_t* at, const uint32_t (&v)[32]) {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        uint32_t q[4];
+#pragma unroll
+                        for (int k = 0; k < 4; ++k)
+                            q[k] = f32x2_to_bf16x2(make_f32x2(__uint_as_float(v[8 * j + 2 * k]), __uint_as_float(v[8 * j + 2 * k + 1])));
+                        *reinterpret_cast<uint4*>(at + (((slot + j) ^ sw) << 4)) = make_uint4(q[0], q[1], q[2], q[3]);
+                    }
+                };
+                if constexpr (FWD) {
+                    if (o.bias) {
+#pragma unroll
+                        for (int j = 0; j < 32; ++j)
+                            if (col + j < o.F) {
+                                g[j] = __float_as_uint(__uint_as_float(g[j]) + __ldg(o.bias + col + j));
+                                u[j] = __float_as_uint(__uint_as_float(u[j]) + __ldg(o.bias + o.F + col + j));
+                            }
+                    }
+                    if (KEEP) { put(box + BOX_BYTES, g); put(box + 2 * BOX_BYTES, u); }
+                    gate_dispatch<false>(o.act, [&](auto a) {
+#pragma unroll
+                        for (int j = 0; j < 32; ++j)
+                            g[j] = __float_as_uint(gate_act<decltype(a)::value, false>(__uint_as_float(g[j])) * __uint_as_float(u[j]));
+                    });
+                }
+                put(box, g);
+            }
+            tc_fence_before_sync();
+            __syncwarp();
+            if (lane == 0) mbar_arrive_cluster(acc_empty0 + buf * 8);
+            if (!there || o.splits > 1) continue;
+            if (p.tma_out) {
+                fence_proxy_async_smem();
+                __syncwarp();
+                if (lane == 0) {
+                    if constexpr (FWD) {
+                        tma_store_2d(&maps.h, boxes, col0, row0);
+                        if (KEEP) { tma_store_2d(&maps.z[0], boxes + BOX_BYTES, col0, row0); tma_store_2d(&maps.z[1], boxes + 2 * BOX_BYTES, col0, row0); }
+                    } else {
+#pragma unroll
+                        for (int b = 0; b < HN / 64; ++b)
+                            if (col0 + b * 64 < o.F) tma_store_2d(&maps.h, boxes + b * BOX_BYTES, col0 + b * 64, row0);
+                    }
+                    bulk_commit();
+                }
+            } else {
+                // rows that TMA cannot address: element by element, the lanes along a row
+#pragma unroll 1
+                for (int b = 0; b < C::BOXES; ++b) {
+                    __nv_bfloat16* const base = static_cast<__nv_bfloat16*>(FWD && b > 0 ? o.z : o.h) + (FWD && b == 2 ? o.F : 0);
+                    const long ld = FWD && b > 0 ? o.ldz : o.ldh;
+                    const int cb = col0 + (FWD ? 0 : b * 64);
+#pragma unroll 4
+                    for (int i = 0; i < 64; ++i) {
+                        const int r = i >> 1, e = (i & 1) * 32 + lane;
+                        const __nv_bfloat16 v = *reinterpret_cast<const __nv_bfloat16*>(boxes + b * BOX_BYTES + r * 128 + (((e >> 3) ^ (r & 7)) << 4) + (e & 7) * 2);
+                        if (row0 + r < o.M && cb + e < o.F) base[(long)(row0 + r) * ld + cb + e] = v;
+                    }
+                }
+                __syncwarp();
+            }
+        }
+        if (lane == 0) bulk_wait();
+    }
+    if (*abort_flag) {
+        for (int i = 0; i < 64; ++i) __nanosleep(1000);
+    }
+    tc_fence_before_sync();
+    cluster_sync_all();
+    if (warp == 1) { tc_fence_after_sync(); tmem_dealloc_pair(tmem_base, 512); }
+}
+}  // namespace tc
+}  // namespace dpclip

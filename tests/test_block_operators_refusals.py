@@ -161,6 +161,28 @@ def test_qknorm_refusals(own):
         assert r(*args, None) == INVALID, args
 
 
+def test_gated_refusals(own):
+    f, b = own.dpclip_gated_forward, own.dpclip_gated_backward
+    f.argtypes = [vp, i64, vp, i64, vp, i32, i32, i32, i32, i32, vp, i64, vp, i64, vp, ctypes.c_size_t, vp]
+    good = [at(0x1000), 64, at(0x2000), 64, at(0x3000), 16, 64, 32, 1, 0, at(0x4000), 32, at(0x5000), 64, at(0x10000), 1 << 30, None]
+    for pos, value, want in ((0, None, INVALID), (2, None, INVALID), (10, None, INVALID), (1, 63, INVALID), (3, 63, INVALID), (11, 31, INVALID),
+                             (13, 63, INVALID), (5, 0, INVALID), (6, 0, INVALID), (7, 0, INVALID), (8, 2, INVALID), (9, 4, INVALID), (9, -1, INVALID),
+                             (0, at(0x1001), MISALIGNED), (2, at(0x2001), MISALIGNED), (4, at(0x3002), MISALIGNED), (10, at(0x4001), MISALIGNED),
+                             (12, at(0x5001), MISALIGNED), (14, None, WORKSPACE), (14, at(0x10010), WORKSPACE), (15, 255, WORKSPACE)):
+        args = list(good)
+        args[pos] = value
+        assert f(*args) == want, (pos, value)
+    b.argtypes = [vp, i64, vp, i64, vp, i64, i32, i32, i32, i32, i32, vp, i64, vp, i64, vp, ctypes.c_size_t, vp]
+    good = [at(0x1000), 32, at(0x2000), 64, at(0x3000), 64, 16, 64, 32, 1, 0, at(0x4000), 64, at(0x5000), 64, at(0x10000), 1 << 30, None]
+    for pos, value, want in ((0, None, INVALID), (2, None, INVALID), (4, None, INVALID), (11, None, INVALID), (1, 31, INVALID), (3, 63, INVALID),
+                             (5, 63, INVALID), (12, 63, INVALID), (14, 63, INVALID), (6, 0, INVALID), (7, 0, INVALID), (8, 0, INVALID), (9, 7, INVALID),
+                             (10, 9, INVALID), (0, at(0x1001), MISALIGNED), (2, at(0x2001), MISALIGNED), (4, at(0x3001), MISALIGNED),
+                             (11, at(0x4001), MISALIGNED), (13, at(0x5001), MISALIGNED), (15, None, WORKSPACE), (16, 255, WORKSPACE)):
+        args = list(good)
+        args[pos] = value
+        assert b(*args) == want, (pos, value)
+
+
 def test_host_tensors_are_refused(dp):
     """The library reads device memory: a tensor of the host never reaches it."""
     import torch
