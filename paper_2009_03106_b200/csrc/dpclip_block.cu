@@ -336,7 +336,7 @@ int launch_gated_tc(const tc::gt::Maps& maps, const tc::gt::Params& p, cudaStrea
     if (cudaFuncSetAttribute(tc::gated_tc_kernel<FWD, KEEP, HN>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM_BYTES) != cudaSuccess)
         return DPCLIP_ERR_CUDA;
     const int pairs = p.total < kPairs ? p.total : kPairs;
-    tc::gated_tc_kernel<FWD, KEEP, HN><<<2 * pairs, tc::gt::THREADS, C::SMEM_BYTES, st>>>(maps, p);
+    tc::gated_tc_kernel<FWD, KEEP, HN><<<2 * pairs, C::THREADS, C::SMEM_BYTES, st>>>(maps, p);
     const int rc = finish_launch();
     return rc || p.out.splits == 1 ? rc : launch_gated_reduce<__nv_bfloat16, FWD>(p.out, st);
 }

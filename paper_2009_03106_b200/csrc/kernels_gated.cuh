@@ -6,7 +6,7 @@
 //                        lies side by side in each CTA's tensor memory, so that activation and product are the epilogue.  Backward: the
 //                        plain product dZ W, with W read as it lies (its contraction index is the row: MN-major operand).
 //   gated_simt_kernel    the same two products on the fp32 ALUs: fp32 inputs, and rows that TMA cannot address.
-//   gated_few_kernel     up to eight rows of X: the weights are streamed once, a warp takes two gate and two up rows.
+//   gated_few_kernel     up to eight rows of X: the weights are streamed once, a warp takes one gate row and its up row.
 //   gated_reduce_kernel  adds up the partial products of a split contraction, in order, and ends as the products' epilogue does.
 //   gated_signal_kernel  dh, z -> dz: five passes over M x F numbers, bound by memory.
 //
@@ -49,6 +49,31 @@ template <int ACT, bool EXACT> __device__ __forceinline__ void gate_act_grad(flo
         const float p = gate_sigmoid<EXACT>(2.f * kGeluTanh * z * fmaf(kGeluCube * z, z, 1.f));
         a = z * p;
         da = fmaf(a * (1.f - p), 2.f * kGeluTanh * fmaf(3.f * kGeluCube * z, z, 1.f), p);
+    }
+}
+// act(g) (.) u of a pair, for bf16 results: sigmoid(s) = 1 / (1 + 2^(-s log2 e)), each of the two by the hardware's approximation (2^-22).  The
+// epilogue of the tensor-core kernel is made of little else (per element two of them and three multiply-adds; one element at a time, with
+// __expf and __fdividef, it was 21 instructions and bound the kernel).
+__device__ __forceinline__ float gate_ex2(float x) { float r; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x)); return r; }
+__device__ __forceinline__ float gate_rcp(float x) { float r; asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x)); return r; }
+constexpr float kLog2e = 1.4426950408889634f;
+template <int ACT> __device__ __forceinline__ f32x2 gate_pair(f32x2 g, f32x2 u) {
+    if constexpr (ACT == DPCLIP_ACT_SILU || ACT == DPCLIP_ACT_GELU_TANH) {
+        f32x2 e;
+        if constexpr (ACT == DPCLIP_ACT_SILU) e = mul2(g, make_f32x2(-kLog2e, -kLog2e));
+        else {
+            constexpr float a = -2.f * kGeluTanh * kLog2e, b = a * kGeluCube;
+            e = mul2(g, fma2(mul2(g, g), make_f32x2(b, b), make_f32x2(a, a)));
+        }
+        float x, y;
+        split_f32x2(e, x, y);
+        split_f32x2(add2(make_f32x2(gate_ex2(x), gate_ex2(y)), make_f32x2(1.f, 1.f)), x, y);
+        return mul2(mul2(g, u), make_f32x2(gate_rcp(x), gate_rcp(y)));
+    } else {
+        float a, b, c, d;
+        split_f32x2(g, a, b);
+        split_f32x2(u, c, d);
+        return make_f32x2(gate_act<ACT, false>(a) * c, gate_act<ACT, false>(b) * d);
     }
 }
 template <bool EXACT, typename F> __device__ __forceinline__ void gate_dispatch(int act, F f) {
@@ -179,7 +204,7 @@ struct GatedSimt {
     GatedOut out;
 };
 template <typename T, bool FWD, int BM>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(256, 2)
 gated_simt_kernel(const __grid_constant__ GatedSimt p) {
     constexpr int BN = 128, BK = 16, RM = BM / 16, LA = BM * BK / 256, LB = BN * BK / 256, HALF = FWD ? 64 : 128;
     __shared__ __align__(16) float as[2][BK][BM + 4], bs[2][BK][BN + 4];
@@ -216,12 +241,12 @@ gated_simt_kernel(const __grid_constant__ GatedSimt p) {
             else bs[b][(tid >> 7) + 2 * i][tid & 127] = rb[i];
         }
     };
-    // thread's rows: ty * 4 + r and 64 + ty * 4 + r (BM = 128), or ty * 2 + r (BM = 32); columns: tx * 4 + c and 64 + tx * 4 + c
-    float acc[RM][8];
+    // thread's rows: ty * 4 + r and 64 + ty * 4 + r (BM = 128), or ty * 2 + r (BM = 32); columns: tx * 4 + c and 64 + tx * 4 + c, in pairs
+    f32x2 acc2[RM][4];
 #pragma unroll
     for (int r = 0; r < RM; ++r)
 #pragma unroll
-        for (int c = 0; c < 8; ++c) acc[r][c] = 0.f;
+        for (int c = 0; c < 4; ++c) acc2[r][c] = make_f32x2(0.f, 0.f);
     fetch(k_begin);
     put(0);
     __syncthreads();
@@ -231,7 +256,8 @@ gated_simt_kernel(const __grid_constant__ GatedSimt p) {
         if (more) fetch(k0 + BK);
 #pragma unroll
         for (int k = 0; k < BK; ++k) {
-            float x[RM], y[8];
+            float x[RM];
+            f32x2 y[4];
             if constexpr (RM == 8) {
                 const float4 u = *reinterpret_cast<const float4*>(&as[buf][k][ty * 4]), v = *reinterpret_cast<const float4*>(&as[buf][k][64 + ty * 4]);
                 x[0] = u.x; x[1] = u.y; x[2] = u.z; x[3] = u.w; x[4] = v.x; x[5] = v.y; x[6] = v.z; x[7] = v.w;
@@ -240,11 +266,13 @@ gated_simt_kernel(const __grid_constant__ GatedSimt p) {
                 x[0] = u.x; x[1] = u.y;
             }
             const float4 u = *reinterpret_cast<const float4*>(&bs[buf][k][tx * 4]), v = *reinterpret_cast<const float4*>(&bs[buf][k][64 + tx * 4]);
-            y[0] = u.x; y[1] = u.y; y[2] = u.z; y[3] = u.w; y[4] = v.x; y[5] = v.y; y[6] = v.z; y[7] = v.w;
+            y[0] = make_f32x2(u.x, u.y); y[1] = make_f32x2(u.z, u.w); y[2] = make_f32x2(v.x, v.y); y[3] = make_f32x2(v.z, v.w);
 #pragma unroll
-            for (int r = 0; r < RM; ++r)
+            for (int r = 0; r < RM; ++r) {
+                const f32x2 xx = make_f32x2(x[r], x[r]);
 #pragma unroll
-                for (int c = 0; c < 8; ++c) acc[r][c] = fmaf(x[r], y[c], acc[r][c]);
+                for (int c = 0; c < 4; ++c) acc2[r][c] = fma2(xx, y[c], acc2[r][c]);
+            }
         }
         if (more) put(buf ^ 1);
         buf ^= 1;
@@ -254,6 +282,9 @@ gated_simt_kernel(const __grid_constant__ GatedSimt p) {
     for (int r = 0; r < RM; ++r) {
         const int m = m0 + (RM == 8 ? (r >> 2) * 64 + ty * 4 + (r & 3) : ty * 2 + r);
         if (m >= p.M) continue;
+        float acc[8];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) split_f32x2(acc2[r][c], acc[2 * c], acc[2 * c + 1]);
         if constexpr (FWD) {
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
@@ -261,9 +292,9 @@ gated_simt_kernel(const __grid_constant__ GatedSimt p) {
                 if (f >= p.N) continue;
                 if (p.out.splits > 1) {
                     float* to = p.out.part + ((long)blockIdx.y * p.M + m) * 2 * p.N + f;
-                    to[0] = acc[r][c]; to[p.N] = acc[r][c + 4];
+                    to[0] = acc[c]; to[p.N] = acc[c + 4];
                 } else {
-                    gated_end<T>(p.out, m, f, acc[r][c], acc[r][c + 4]);
+                    gated_end<T>(p.out, m, f, acc[c], acc[c + 4]);
                 }
             }
         } else {
@@ -271,8 +302,8 @@ gated_simt_kernel(const __grid_constant__ GatedSimt p) {
             for (int c = 0; c < 8; ++c) {
                 const int n = n0 + (c >> 2) * 64 + tx * 4 + (c & 3);
                 if (n >= p.N) continue;
-                if (p.out.splits > 1) p.out.part[((long)blockIdx.y * p.M + m) * p.N + n] = acc[r][c];
-                else gate_store(static_cast<T*>(p.out.h) + (long)m * p.out.ldh + n, acc[r][c]);
+                if (p.out.splits > 1) p.out.part[((long)blockIdx.y * p.M + m) * p.N + n] = acc[c];
+                else gate_store(static_cast<T*>(p.out.h) + (long)m * p.out.ldh + n, acc[c]);
             }
         }
     }
@@ -297,7 +328,7 @@ template <typename T, int V> __device__ __forceinline__ void gated_vec(const T* 
         for (int k = 0; k < 4; ++k) { x[2 * k] = __uint_as_float(w[k] << 16); x[2 * k + 1] = __uint_as_float(w[k] & 0xFFFF0000u); }
     }
 }
-constexpr int GF_ROWS = 2;               // gate rows of W a warp, and as many up rows
+constexpr int GF_ROWS = 1;               // gate rows of W a warp, and as many up rows
 template <typename T, int V, int MT>
 __global__ void __launch_bounds__(128)
 gated_few_kernel(const __grid_constant__ GatedFew p) {
@@ -316,7 +347,7 @@ gated_few_kernel(const __grid_constant__ GatedFew p) {
     for (int r = 0; r < 2 * GF_ROWS; ++r)
 #pragma unroll
         for (int m = 0; m < MT; ++m) acc[r][m] = 0.f;
-#pragma unroll 2
+#pragma unroll 4
     for (int k = lane * V; k < p.K; k += 32 * V) {
         float w[2 * GF_ROWS][V];
 #pragma unroll
@@ -353,13 +384,15 @@ namespace tc {
 namespace gt {
 constexpr int BK = 64, BM_CTA = 128;
 constexpr int A_BYTES = BM_CTA * 128;                    // 128 rows x 64 bf16
-constexpr int EPI_WARPS = 8, THREADS = 64 + 32 * EPI_WARPS;
 constexpr int BOX_BYTES = 32 * 128;                      // 32 rows x 64 bf16 of an output
-// boxes of outputs a warp stages: forward h (and zg, zu) of its 32 rows x 64 columns; backward 32 rows x 2 HN / 2 columns
+// Epilogue warps and the boxes of outputs they stage.  Forward: 16 warps, each 32 rows x 32 columns of h (and of zg, zu); two neighbours fill a
+// box together.  (With 8 warps of 64 columns the epilogue's latency, not its 0.24 of the issue slots, paced the kernel: 133 us.)  Backward: 8
+// warps, each 32 rows x HN columns of dx.
 template <bool FWD, bool KEEP, int HN> struct Cfg {
-    static constexpr int BOXES = FWD ? (KEEP ? 3 : 1) : HN / 64;
+    static constexpr int EPI_WARPS = FWD ? 16 : 8, THREADS = 64 + 32 * EPI_WARPS;
+    static constexpr int BOXES = FWD ? (KEEP ? 3 : 1) : HN / 64;         // of a pair of warps, or of a warp
     static constexpr int STAGE_BYTES = A_BYTES + HN * 128;
-    static constexpr int STAGING = EPI_WARPS * BOXES * BOX_BYTES;
+    static constexpr int STAGING = 8 * BOXES * BOX_BYTES;
     static constexpr int STAGES = (224 * 1024 - STAGING) / STAGE_BYTES;
     static constexpr int SMEM_BYTES = STAGES * STAGE_BYTES + STAGING + 256 + 1024;
 };
@@ -402,10 +435,10 @@ __device__ __forceinline__ void bulk_wait() { asm volatile("cp.async.bulk.wait_g
 }  // namespace gt
 
 // Warp 0: loads of this CTA's operands (A rows; gate or up rows of W, or half of the columns of W), all counted on CTA 0's `full`; warp 1 of
-// CTA 0: MMAs, commits to both CTAs' `empty` and `acc_full`; eight epilogue warps a CTA: two for each quarter of the tensor-memory lanes.
+// CTA 0: MMAs, commits to both CTAs' `empty` and `acc_full`; the others: epilogue, warp w on lanes 32 (w % 4) .. + 31 of the tensor memory.
 // The accumulator is double-buffered (2 x 2 HN <= 512 columns), so a tile's epilogue runs under the next tile's MMAs.  Every wait is bounded.
 template <bool FWD, bool KEEP, int HN>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(gt::THREADS, 1)
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__((gt::Cfg<FWD, KEEP, HN>::THREADS), 1)
 gated_tc_kernel(const __grid_constant__ gt::Maps maps, const __grid_constant__ gt::Params p) {
     using namespace gt;
     using C = Cfg<FWD, KEEP, HN>;
@@ -424,7 +457,7 @@ gated_tc_kernel(const __grid_constant__ gt::Maps maps, const __grid_constant__ g
     const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
     if (threadIdx.x == 0) {
         for (int s = 0; s < STAGES; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], 1); }
-        for (int b = 0; b < 2; ++b) { mbar_init(&acc_full[b], 1); mbar_init(&acc_empty[b], 2 * EPI_WARPS); }
+        for (int b = 0; b < 2; ++b) { mbar_init(&acc_full[b], 1); mbar_init(&acc_empty[b], 2 * C::EPI_WARPS); }
         *abort_flag = 0;
         mbar_fence_init();
         tma_prefetch_desc(&maps.a); tma_prefetch_desc(&maps.b[rank]);
@@ -493,75 +526,147 @@ gated_tc_kernel(const __grid_constant__ gt::Maps maps, const __grid_constant__ g
                 mma_commit_pair(&acc_full[buf], 3);
             }
         }
-    } else {
-        const int quarter = warp & 3, half = (warp - 2) >> 2;
-        uint8_t* const boxes = staging + (warp - 2) * C::BOXES * BOX_BYTES;
+    } else if constexpr (FWD) {
+        // ------------------------------------------------ epilogue, forward: 32 columns a warp
+        const int quarter = warp & 3, group = (warp - 2) >> 2, box = group >> 1, slot = (group & 1) * 4;
+        uint8_t* const boxes = staging + (box * 4 + quarter) * C::BOXES * BOX_BYTES;
+        const int pair_bar = 1 + box * 4 + quarter;                          // the two warps of a box
+        const bool stores = (group & 1) == 0 && lane == 0;                   // who hands the box to TMA
         const uint32_t acc_empty0 = mapa_shared(smem_u32(acc_empty), 0);
         const GatedOut& o = p.out;
-        // forward: a warp has 64 columns of h (the second half of the warps only when HN = 128); backward: HN columns of dx
-        constexpr int CHUNKS = FWD ? 2 : HN / 32;
-        const bool mine = !FWD || HN == 128 || half == 0;
-        const int c0 = FWD ? half * 64 : half * HN;                          // first column within the tile
         int it = 0;
         for (int t = pair; t < p.total; t += pairs, ++it) {
             const Tile w = tile_at(p, t);
             const int buf = it & 1;
             const int row0 = w.m * 2 * BM_CTA + (int)rank * BM_CTA + quarter * 32;
-            const int col0 = w.n * (FWD ? HN : N) + c0;
+            const int box_col = w.n * HN + box * 64, col = box_col + (group & 1) * 32;
             if (!mbar_wait(&acc_full[buf], (it >> 1) & 1, abort_flag, p.status)) break;
             tc_fence_after_sync();
-            const uint32_t tm = tmem_base + ((uint32_t)(quarter * 32) << 16) + buf * N + c0;
-            const bool there = mine && row0 < o.M && col0 < o.F;
+            const uint32_t tm = tmem_base + ((uint32_t)(quarter * 32) << 16) + buf * N + group * 32;
+            const bool there = group * 32 < HN && row0 < o.M && box_col < o.F;   // the same for both warps of a box
+            uint32_t g[32], u[32];
+            if (there) {
+                tmem_ld_32x32(tm, g);
+                tmem_ld_32x32(tm + HN, u);
+                tmem_ld_wait();
+            }
+            tc_fence_before_sync();
+            __syncwarp();
+            if (lane == 0) mbar_arrive_cluster(acc_empty0 + buf * 8);
+            if (!there) continue;
+            if (o.splits > 1) {
+                // partial products: a thread's row, 128 bytes of it
+                const int m = row0 + lane;
+                if (m < o.M) {
+                    float* to = o.part + ((long)w.split * o.M + m) * 2L * o.F + col;
+#pragma unroll
+                    for (int j = 0; j < 32; ++j)
+                        if (col + j < o.F) { to[j] = __uint_as_float(g[j]); to[o.F + j] = __uint_as_float(u[j]); }
+                }
+                continue;
+            }
+            if (stores) bulk_wait_read();                                    // the box's last tile has left
+            asm volatile("bar.sync %0, 64;" ::"r"(pair_bar) : "memory");
+            // 32 columns of a row = four 16-byte slots of a 128-byte row, at their swizzled places
+            uint8_t* const mine = boxes + lane * 128;
+            const int sw = lane & 7;
+            auto put = [&](uint8_t* at, const uint32_t (&v)[32]) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    uint32_t q[4];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        q[k] = f32x2_to_bf16x2(make_f32x2(__uint_as_float(v[8 * j + 2 * k]), __uint_as_float(v[8 * j + 2 * k + 1])));
+                    *reinterpret_cast<uint4*>(at + (((slot + j) ^ sw) << 4)) = make_uint4(q[0], q[1], q[2], q[3]);
+                }
+            };
+            if (o.bias) {
+#pragma unroll
+                for (int j = 0; j < 32; ++j)
+                    if (col + j < o.F) {
+                        g[j] = __float_as_uint(__uint_as_float(g[j]) + __ldg(o.bias + col + j));
+                        u[j] = __float_as_uint(__uint_as_float(u[j]) + __ldg(o.bias + o.F + col + j));
+                    }
+            }
+            if (KEEP) { put(mine + BOX_BYTES, g); put(mine + 2 * BOX_BYTES, u); }
+            gate_dispatch<false>(o.act, [&](auto a) {
+#pragma unroll
+                for (int j = 0; j < 32; j += 2) {
+                    const f32x2 h = gate_pair<decltype(a)::value>(make_f32x2(__uint_as_float(g[j]), __uint_as_float(g[j + 1])),
+                                                                  make_f32x2(__uint_as_float(u[j]), __uint_as_float(u[j + 1])));
+                    float x, y;
+                    split_f32x2(h, x, y);
+                    g[j] = __float_as_uint(x); g[j + 1] = __float_as_uint(y);
+                }
+            });
+            put(mine, g);
+            if (p.tma_out) fence_proxy_async_smem();
+            asm volatile("bar.sync %0, 64;" ::"r"(pair_bar) : "memory");
+            if (p.tma_out) {
+                if (stores) {
+                    tma_store_2d(&maps.h, boxes, box_col, row0);
+                    if (KEEP) { tma_store_2d(&maps.z[0], boxes + BOX_BYTES, box_col, row0); tma_store_2d(&maps.z[1], boxes + 2 * BOX_BYTES, box_col, row0); }
+                    bulk_commit();
+                }
+            } else {
+                // rows that TMA cannot address: element by element, the lanes along a row; each warp its own 32 columns
+#pragma unroll 1
+                for (int b = 0; b < C::BOXES; ++b) {
+                    __nv_bfloat16* const base = static_cast<__nv_bfloat16*>(b > 0 ? o.z : o.h) + (b == 2 ? o.F : 0);
+                    const long ld = b > 0 ? o.ldz : o.ldh;
+                    const int e = (group & 1) * 32 + lane;
+#pragma unroll 4
+                    for (int r = 0; r < 32; ++r) {
+                        const __nv_bfloat16 v = *reinterpret_cast<const __nv_bfloat16*>(boxes + b * BOX_BYTES + r * 128 + (((e >> 3) ^ (r & 7)) << 4) + (e & 7) * 2);
+                        if (row0 + r < o.M && col + lane < o.F) base[(long)(row0 + r) * ld + col + lane] = v;
+                    }
+                }
+            }
+        }
+        if (stores) bulk_wait();
+    } else {
+        // ------------------------------------------------ epilogue, backward: HN columns a warp
+        const int quarter = warp & 3, half = (warp - 2) >> 2;
+        uint8_t* const boxes = staging + (warp - 2) * C::BOXES * BOX_BYTES;
+        const uint32_t acc_empty0 = mapa_shared(smem_u32(acc_empty), 0);
+        const GatedOut& o = p.out;
+        int it = 0;
+        for (int t = pair; t < p.total; t += pairs, ++it) {
+            const Tile w = tile_at(p, t);
+            const int buf = it & 1;
+            const int row0 = w.m * 2 * BM_CTA + (int)rank * BM_CTA + quarter * 32;
+            const int col0 = w.n * N + half * HN;
+            if (!mbar_wait(&acc_full[buf], (it >> 1) & 1, abort_flag, p.status)) break;
+            tc_fence_after_sync();
+            const uint32_t tm = tmem_base + ((uint32_t)(quarter * 32) << 16) + buf * N + half * HN;
+            const bool there = row0 < o.M && col0 < o.F;
             if (there && o.splits == 1) { if (lane == 0) bulk_wait_read(); __syncwarp(); }
 #pragma unroll 1
-            for (int c = 0; c < CHUNKS; ++c) {
+            for (int c = 0; c < HN / 32; ++c) {
                 if (!there) break;
-                uint32_t g[32], u[32];
+                uint32_t g[32];
                 tmem_ld_32x32(tm + c * 32, g);
-                if (FWD) tmem_ld_32x32(tm + HN + c * 32, u);
                 tmem_ld_wait();
                 const int col = col0 + c * 32;
                 if (o.splits > 1) {
-                    // partial products: a thread's row, 128 bytes of it
                     const int m = row0 + lane;
                     if (m < o.M) {
-                        float* to = o.part + ((long)w.split * o.M + m) * (FWD ? 2L * o.F : o.F) + col;
+                        float* to = o.part + ((long)w.split * o.M + m) * o.F + col;
 #pragma unroll
-                        for (int j = 0; j < 32; ++j)
-                            if (col + j < o.F) { to[j] = __uint_as_float(g[j]); if (FWD) to[o.F + j] = __uint_as_float(u[j]); }
+                        for (int j = 0; j < 32; ++j) if (col + j < o.F) to[j] = __uint_as_float(g[j]);
                     }
                     continue;
                 }
-                // 32 columns of a row = four 16-byte slots of a 128-byte row, at their swizzled places
-                uint8_t* const box = boxes + (FWD ? 0 : (c >> 1) * BOX_BYTES) + lane * 128;
+                uint8_t* const at = boxes + (c >> 1) * BOX_BYTES + lane * 128;
                 const int slot = (c & 1) * 4, sw = lane & 7;
-                auto put = [&](uint8_t* at, const uint32_t (&v)[32]) {
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        uint32_t q[4];
+                for (int j = 0; j < 4; ++j) {
+                    uint32_t q[4];
 #pragma unroll
-                        for (int k = 0; k < 4; ++k)
-                            q[k] = f32x2_to_bf16x2(make_f32x2(__uint_as_float(v[8 * j + 2 * k]), __uint_as_float(v[8 * j + 2 * k + 1])));
-                        *reinterpret_cast<uint4*>(at + (((slot + j) ^ sw) << 4)) = make_uint4(q[0], q[1], q[2], q[3]);
-                    }
-                };
-                if constexpr (FWD) {
-                    if (o.bias) {
-#pragma unroll
-                        for (int j = 0; j < 32; ++j)
-                            if (col + j < o.F) {
-                                g[j] = __float_as_uint(__uint_as_float(g[j]) + __ldg(o.bias + col + j));
-                                u[j] = __float_as_uint(__uint_as_float(u[j]) + __ldg(o.bias + o.F + col + j));
-                            }
-                    }
-                    if (KEEP) { put(box + BOX_BYTES, g); put(box + 2 * BOX_BYTES, u); }
-                    gate_dispatch<false>(o.act, [&](auto a) {
-#pragma unroll
-                        for (int j = 0; j < 32; ++j)
-                            g[j] = __float_as_uint(gate_act<decltype(a)::value, false>(__uint_as_float(g[j])) * __uint_as_float(u[j]));
-                    });
+                    for (int k = 0; k < 4; ++k)
+                        q[k] = f32x2_to_bf16x2(make_f32x2(__uint_as_float(g[8 * j + 2 * k]), __uint_as_float(g[8 * j + 2 * k + 1])));
+                    *reinterpret_cast<uint4*>(at + (((slot + j) ^ sw) << 4)) = make_uint4(q[0], q[1], q[2], q[3]);
                 }
-                put(box, g);
             }
             tc_fence_before_sync();
             __syncwarp();
@@ -571,28 +676,21 @@ gated_tc_kernel(const __grid_constant__ gt::Maps maps, const __grid_constant__ g
                 fence_proxy_async_smem();
                 __syncwarp();
                 if (lane == 0) {
-                    if constexpr (FWD) {
-                        tma_store_2d(&maps.h, boxes, col0, row0);
-                        if (KEEP) { tma_store_2d(&maps.z[0], boxes + BOX_BYTES, col0, row0); tma_store_2d(&maps.z[1], boxes + 2 * BOX_BYTES, col0, row0); }
-                    } else {
 #pragma unroll
-                        for (int b = 0; b < HN / 64; ++b)
-                            if (col0 + b * 64 < o.F) tma_store_2d(&maps.h, boxes + b * BOX_BYTES, col0 + b * 64, row0);
-                    }
+                    for (int b = 0; b < HN / 64; ++b)
+                        if (col0 + b * 64 < o.F) tma_store_2d(&maps.h, boxes + b * BOX_BYTES, col0 + b * 64, row0);
                     bulk_commit();
                 }
             } else {
-                // rows that TMA cannot address: element by element, the lanes along a row
 #pragma unroll 1
                 for (int b = 0; b < C::BOXES; ++b) {
-                    __nv_bfloat16* const base = static_cast<__nv_bfloat16*>(FWD && b > 0 ? o.z : o.h) + (FWD && b == 2 ? o.F : 0);
-                    const long ld = FWD && b > 0 ? o.ldz : o.ldh;
-                    const int cb = col0 + (FWD ? 0 : b * 64);
+                    __nv_bfloat16* const base = static_cast<__nv_bfloat16*>(o.h);
+                    const int cb = col0 + b * 64;
 #pragma unroll 4
                     for (int i = 0; i < 64; ++i) {
                         const int r = i >> 1, e = (i & 1) * 32 + lane;
                         const __nv_bfloat16 v = *reinterpret_cast<const __nv_bfloat16*>(boxes + b * BOX_BYTES + r * 128 + (((e >> 3) ^ (r & 7)) << 4) + (e & 7) * 2);
-                        if (row0 + r < o.M && cb + e < o.F) base[(long)(row0 + r) * ld + cb + e] = v;
+                        if (row0 + r < o.M && cb + e < o.F) base[(long)(row0 + r) * o.ldh + cb + e] = v;
                     }
                 }
                 __syncwarp();
