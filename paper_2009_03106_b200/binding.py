@@ -8,7 +8,6 @@ from __future__ import annotations
 
 import ctypes
 import os
-import struct
 from dataclasses import dataclass
 from typing import List, Optional, Sequence
 
@@ -131,22 +130,12 @@ def load_library():
     L.dpclip_model_step.restype = _i
     L.dpclip_model_workspace_bytes.argtypes = [ctypes.POINTER(_CModelLayer), _i, _i, _i]
     L.dpclip_model_workspace_bytes.restype = _sz
-    L.dpclip_stored_clipped_grad.argtypes = [_vp, _l, _i, _i, _vp, _vp, _f, _f, _u64, _u64, _vp]
     L.dpclip_relbias_bucket.argtypes = [ctypes.POINTER(_CRelBias), _l]
-    L.dpclip_relbias_forward.argtypes = [_vp, _l, ctypes.POINTER(_CRelBias), _i, _i, _i, _l, _i, _vp, _l, _l, _vp]
-    L.dpclip_relbias_sqnorms.argtypes = [_vp, _l, _l, _l, _i, _i, _i, _i, _l, _vp, _vp, ctypes.POINTER(_CRelBias), _i, _i, _vp, _vp,
-                                         _vp, _sz, _vp]
     L.dpclip_relbias_workspace_bytes.argtypes = [_i] * 6
     L.dpclip_rotation_table.argtypes = [_vp, _l, _i, _d, _d, _vp]
-    qk = [ctypes.c_char_p, _i, _i, _i, _i, _i, _i, _vp, _l, _vp, _l, _f, _i]
-    L.dpclip_qknorm_forward.argtypes = qk + [_vp]
-    L.dpclip_qknorm_backward.argtypes = qk + [ctypes.POINTER(_vp), ctypes.POINTER(_vp), _vp, _sz, _vp]
     L.dpclip_qknorm_workspace_bytes.argtypes = [_i] * 5
-    L.dpclip_gated_forward.argtypes = [_vp, _l, _vp, _l, _vp, _i, _i, _i, _i, _i, _vp, _l, _vp, _l, _vp, _sz, _vp]
-    L.dpclip_gated_backward.argtypes = [_vp, _l, _vp, _l, _vp, _l, _i, _i, _i, _i, _i, _vp, _l, _vp, _l, _vp, _sz, _vp]
     L.dpclip_gated_workspace_bytes.argtypes = [_i] * 4
-    for name in ("dpclip_gated_forward", "dpclip_gated_backward", "dpclip_stored_clipped_grad", "dpclip_relbias_bucket", "dpclip_relbias_forward", "dpclip_relbias_sqnorms",
-                 "dpclip_rotation_table", "dpclip_qknorm_forward", "dpclip_qknorm_backward"):
+    for name in ("dpclip_relbias_bucket", "dpclip_rotation_table"):
         getattr(L, name).restype = _i
     for name in ("dpclip_relbias_workspace_bytes", "dpclip_qknorm_workspace_bytes", "dpclip_gated_workspace_bytes"):
         getattr(L, name).restype = _sz
@@ -814,46 +803,28 @@ def dpclip_step_host(hs: HostStep, C: float, sigma: float, seed: int, stream_id0
 
 
 # ----------------------------------------------------------------------------
-# operators of a transformer block
+# operators of a transformer block: their arguments are checked and marshalled in compiled code (csrc/marshal.cpp)
 # ----------------------------------------------------------------------------
-def _on_device(*tensors: Optional[torch.Tensor]) -> None:
-    """The calls run on the current device: tensors that lie elsewhere are refused."""
-    device = None
-    for t in tensors:
-        if t is not None:
-            at = t.get_device()
-            if at < 0:
-                raise ValueError("expected a CUDA tensor, got one of the host")
-            if device is None:
-                device = _raw_device()
-            if at != device:
-                raise ValueError(f"expected a tensor on the current device {device}, got one on {at}")
+_marshal = None
 
 
-def _dense(t: Optional[torch.Tensor], dtype, shape) -> Optional[int]:
-    """The address of a dense tensor of this type and these sizes (None for None)."""
-    if t is None:
-        return None
-    if t.dtype != dtype or t.shape != shape or not t.is_contiguous():
-        raise ValueError(f"expected a contiguous {dtype} tensor of shape {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
-    return t.data_ptr()
+def _load_marshal():
+    global _marshal
+    load_library()
+    from . import _marshal as m                        # built beside the library, by the same command
+    m.bind(_LIB_PATH)
+    _marshal = m
+    return m
 
 
-def _writable(shape, strides) -> None:
-    """An output's elements have places of their own (no broadcast dimension)."""
-    if 0 in strides and any(s == 0 and n > 1 for s, n in zip(strides, shape)):
-        raise ValueError("an output may not be a broadcast tensor")
+def _handle(stream):
+    return stream if stream is None or isinstance(stream, int) else stream.cuda_stream
 
 
 def dpclip_stored_clipped_grad(grads: torch.Tensor, clip: Optional[torch.Tensor], g: torch.Tensor, sigma: float = 0.0, C: float = 1.0,
                                seed: int = 0, stream_id: int = 0, stream=None) -> None:
     """g = sum_i clip[i] grads[i] (+ noise).  grads (B, ...) dense fp32, g the shape of one example's."""
-    _on_device(grads, clip, g)
-    B, n, f32 = grads.shape[0], g.numel(), torch.float32
-    if grads.numel() != B * n:
-        raise ValueError("g must have the size of one example's gradients")
-    rc = load_library().dpclip_stored_clipped_grad(_dense(grads, f32, grads.shape), n, B, n, _dense(clip, f32, (B,)), _dense(g, f32, g.shape),
-                                                   sigma, C, seed, stream_id, _stream(stream))
+    rc = (_marshal or _load_marshal()).stored_clipped_grad(grads, clip, g, sigma, C, seed, stream_id, _handle(stream))
     if rc:
         raise DpclipError("dpclip_stored_clipped_grad", rc)
 
@@ -869,19 +840,7 @@ def dpclip_relbias_bucket(distance: int, n_buckets: int, max_distance: int, bidi
 def dpclip_relbias_forward(table: torch.Tensor, bias: torch.Tensor, max_distance: int, bidirectional: bool = True, causal: bool = False,
                            q_offset: int = 0, stream=None) -> None:
     """bias (H, Tq, Tk), fp32 or bf16, from table (n_buckets, H) fp32; keys contiguous, other strides free."""
-    _on_device(table, bias)
-    n_buckets, H = table.shape
-    ldt, inner = table.stride()
-    if table.dtype != torch.float32 or (inner != 1 and H > 1):
-        raise ValueError("table must be fp32 with contiguous rows")
-    shape, strides = bias.shape, bias.stride()
-    if len(shape) != 3 or shape[0] != H or (strides[2] != 1 and shape[2] > 1):
-        raise ValueError(f"bias must be (H={H}, Tq, Tk) with contiguous keys, got {tuple(shape)}")
-    _writable(shape, strides)
-    _, Tq, Tk = shape
-    rc = load_library().dpclip_relbias_forward(
-        table.data_ptr(), ldt if n_buckets > 1 else H, _CRelBias(n_buckets, max_distance, bidirectional, causal), H, Tq, Tk, q_offset,
-        _dtype_code(bias), bias.data_ptr(), strides[1] if Tq > 1 else Tk, strides[0], _stream(stream))
+    rc = (_marshal or _load_marshal()).relbias_forward(table, bias, max_distance, bidirectional, causal, q_offset, _handle(stream))
     if rc:
         raise DpclipError("dpclip_relbias_forward", rc)
 
@@ -894,62 +853,20 @@ def dpclip_relbias_sqnorms(dS: torch.Tensor, grads: torch.Tensor, sq_layer: torc
                            bidirectional: bool = True, causal: bool = False, q_offset: int = 0, q_lens: Optional[torch.Tensor] = None,
                            k_lens: Optional[torch.Tensor] = None, accumulate: bool = False, stream=None) -> None:
     """From dS (B, H, Tq, Tk), keys contiguous: grads (B, n_buckets, H) and sq_layer (B,), the squared norms of its rows."""
-    _on_device(dS, grads, sq_layer, workspace, q_lens, k_lens)
-    B, H, Tq, Tk = dS.shape
-    example, head, row, key = dS.stride()
-    if key != 1 and Tk > 1:
-        raise ValueError("keys of dS must be contiguous")
-    n_buckets, f32, i32 = grads.shape[1], torch.float32, torch.int32
-    rc = load_library().dpclip_relbias_sqnorms(
-        dS.data_ptr(), row if Tq > 1 else Tk, head, example, B, H, Tq, Tk, q_offset, _dense(q_lens, i32, (B,)), _dense(k_lens, i32, (B,)),
-        _CRelBias(n_buckets, max_distance, bidirectional, causal), _dtype_code(dS), accumulate, _dense(grads, f32, (B, n_buckets, H)),
-        _dense(sq_layer, f32, (B,)), workspace.data_ptr(), workspace.nbytes, _stream(stream))
+    rc = (_marshal or _load_marshal()).relbias_sqnorms(dS, grads, sq_layer, workspace, max_distance, bidirectional, causal, q_offset, q_lens, k_lens,
+                                                       accumulate, _handle(stream))
     if rc:
         raise DpclipError("dpclip_relbias_sqnorms", rc)
 
 
 def dpclip_rotation_table(table: torch.Tensor, base: float = 10000.0, scale: float = 1.0, stream=None) -> None:
     """table (n_pos, 2, rot_dim / 2) fp32: cosines and sines of every position's angles."""
-    _on_device(table)
     n_pos, two, half = table.shape
-    if two != 2:
-        raise ValueError("table must be (n_pos, 2, rot_dim / 2)")
-    _check("dpclip_rotation_table", load_library().dpclip_rotation_table(_dense(table, torch.float32, table.shape), n_pos, 2 * half, base, scale,
-                                                                         _stream(stream)))
-
-
-# dpclip_heads as packed bytes, one or two of them (a ctypes structure of this size takes 2 us to fill)
-_HEADS = "PlllPlllPllliP"
-_heads_pack = (None, struct.Struct("@" + _HEADS).pack, struct.Struct("@" + _HEADS + _HEADS).pack)
-
-
-def _heads(x, gain, out, dy, shape, dtype):
-    """One descriptor's fields: (B, T, H, D) tensors with a contiguous last dimension."""
-    B, T, H, D = x.shape
-    sx, so = x.stride(), out.stride()
-    fine = (B, T, D) == shape and x.dtype == dtype and out.dtype == dtype and out.shape == x.shape and (D == 1 or sx[3] == so[3] == 1)
-    if dy is not None:
-        sd = dy.stride()
-        fine = fine and dy.dtype == dtype and dy.shape == x.shape and (D == 1 or sd[3] == 1)
-    if not fine:
-        raise ValueError(f"expected {dtype} tensors (B, T, H, D) = ({shape[0]}, {shape[1]}, H, {shape[2]}) with contiguous heads")
-    _writable(out.shape, so)
-    g = 0 if gain is None else _dense(gain, torch.float32, (D,))
-    if dy is None:
-        return x.data_ptr(), sx[0], sx[1], sx[2], 0, 0, 0, 0, out.data_ptr(), so[0], so[1], so[2], H, g
-    return x.data_ptr(), sx[0], sx[1], sx[2], dy.data_ptr(), sd[0], sd[1], sd[2], out.data_ptr(), so[0], so[1], so[2], H, g
-
-
-def _angles(rotation: Optional[torch.Tensor], rot_dim: Optional[int], positions: Optional[torch.Tensor], B: int, T: int):
-    pos = None if positions is None else _dense(positions, torch.int32, (B, T))
-    if rotation is None:
-        if rot_dim:
-            raise ValueError("rot_dim needs a table of angles")
-        return None, 0, 1 << 62, pos
-    n_pos, two, half = rotation.shape
-    if two != 2 or (rot_dim is not None and rot_dim != 2 * half):
-        raise ValueError(f"expected angles (n_pos, 2, rot_dim / 2) for rot_dim {rot_dim}, got {tuple(rotation.shape)}")
-    return _dense(rotation, torch.float32, rotation.shape), 2 * half, n_pos, pos
+    if two != 2 or table.dtype != torch.float32 or not table.is_contiguous() or not table.is_cuda:
+        raise ValueError("table must be a contiguous fp32 CUDA tensor (n_pos, 2, rot_dim / 2)")
+    if table.get_device() != _raw_device():
+        raise ValueError("table must lie on the current device")
+    _check("dpclip_rotation_table", load_library().dpclip_rotation_table(_ptr(table), n_pos, 2 * half, base, scale, _stream(stream)))
 
 
 def dpclip_qknorm_forward(q: torch.Tensor, k: Optional[torch.Tensor], gain_q: Optional[torch.Tensor], gain_k: Optional[torch.Tensor],
@@ -958,14 +875,8 @@ def dpclip_qknorm_forward(q: torch.Tensor, k: Optional[torch.Tensor], gain_q: Op
                           eps: float = 1e-6, stream=None) -> None:
     """q (B, T, Hq, D) and k (B, T, Hk, D) or None, any strides with contiguous heads; rotation (n_pos, 2, rot_dim / 2); positions (B, T)
     int32 or None (pos0 + t)."""
-    _on_device(q, k, gain_q, gain_k, rotation, q_out, k_out, positions)
-    B, T, _, D = q.shape
-    fields, n = _heads(q, gain_q, q_out, None, (B, T, D), q.dtype), 1
-    if k is not None:
-        fields, n = fields + _heads(k, gain_k, k_out, None, (B, T, D), q.dtype), 2
-    table, rot, n_pos, pos = _angles(rotation, rot_dim, positions, B, T)
-    rc = load_library().dpclip_qknorm_forward(_heads_pack[n](*fields), n, B, T, D, rot, interleaved, table, n_pos, pos, pos0, eps,
-                                              _dtype_code(q), _stream(stream))
+    rc = (_marshal or _load_marshal()).qknorm_forward(q, k, gain_q, gain_k, rotation, q_out, k_out, rot_dim, interleaved, positions, pos0, eps,
+                                                      _handle(stream))
     if rc:
         raise DpclipError("dpclip_qknorm_forward", rc)
 
@@ -981,34 +892,10 @@ def dpclip_qknorm_backward(dq_out: torch.Tensor, dk_out: Optional[torch.Tensor],
                            rot_dim: Optional[int] = None, interleaved: bool = False, positions: Optional[torch.Tensor] = None, pos0: int = 0,
                            eps: float = 1e-6, stream=None) -> None:
     """Signals dq, dk at the inputs, per-example gradients of the gains (B, D) and their squared norms (B,)."""
-    _on_device(dq_out, dk_out, q, k, gain_q, gain_k, rotation, dq, dk, grads_q, grads_k, sq_q, sq_k, workspace, positions)
-    B, T, _, D = q.shape
-    fields, n = _heads(q, gain_q, dq, dq_out, (B, T, D), q.dtype), 1
-    if k is not None:
-        fields, n = fields + _heads(k, gain_k, dk, dk_out, (B, T, D), q.dtype), 2
-    table, rot, n_pos, pos = _angles(rotation, rot_dim, positions, B, T)
-    f32 = torch.float32
-    grads = (_vp * 2)(_dense(grads_q, f32, (B, D)), _dense(grads_k, f32, (B, D)))
-    sq = (_vp * 2)(_dense(sq_q, f32, (B,)), _dense(sq_k, f32, (B,)))
-    rc = load_library().dpclip_qknorm_backward(_heads_pack[n](*fields), n, B, T, D, rot, interleaved, table, n_pos, pos, pos0, eps,
-                                               _dtype_code(q), grads, sq, workspace.data_ptr(), workspace.nbytes, _stream(stream))
+    rc = (_marshal or _load_marshal()).qknorm_backward(dq_out, dk_out, q, k, gain_q, gain_k, rotation, dq, dk, grads_q, grads_k, sq_q, sq_k, workspace,
+                                                       rot_dim, interleaved, positions, pos0, eps, _handle(stream))
     if rc:
         raise DpclipError("dpclip_qknorm_backward", rc)
-
-
-def _matrix(t: torch.Tensor, dtype, rows: Optional[int], cols: Optional[int]):
-    """A (..., columns) tensor as a matrix of equally spaced rows: (address, row stride, rows, columns)."""
-    if t.dim() == 2:
-        M, n = t.shape
-        ld, inner = t.stride()
-        if M == 1:
-            ld = n
-    else:
-        B, T, n, ld = _rows(t)
-        M, inner = B * T, 1
-    if t.dtype != dtype or (rows is not None and M != rows) or (cols is not None and n != cols) or (inner != 1 and n > 1):
-        raise ValueError(f"expected {dtype} rows ({rows}, {cols}) with contiguous columns, got {t.dtype} {tuple(t.shape)}")
-    return t.data_ptr(), ld, M, n
 
 
 def dpclip_gated_workspace_bytes(M: int, K: int, F: int, dtype: int = DPCLIP_F32) -> int:
@@ -1019,45 +906,14 @@ def dpclip_gated_forward(X: torch.Tensor, W: torch.Tensor, bias: Optional[torch.
                          act: int, workspace: torch.Tensor, stream=None) -> None:
     """H = act(X Wg^T + bg) (.) (X Wu^T + bu).  X (..., K), W (2F, K) gate rows first, bias (2F,) fp32 or None, H (..., F), Z (..., 2F) or
     None (the pre-activations, for dpclip_gated_backward)."""
-    _on_device(X, W, bias, H, Z, workspace)
-    dt = X.dtype
-    x, ldx, M, K = _matrix(X, dt, None, None)
-    w, ldw, F2, _ = _matrix(W, dt, None, K)
-    F = F2 // 2
-    if F2 % 2:
-        raise ValueError("W must have an even number of rows: gate rows, then up rows")
-    h, ldh, _, _ = _matrix(H, dt, M, F)
-    _writable(H.shape, H.stride())
-    z, ldz = None, 0
-    if Z is not None:
-        z, ldz, _, _ = _matrix(Z, dt, M, F2)
-        _writable(Z.shape, Z.stride())
-    rc = load_library().dpclip_gated_forward(x, ldx, w, ldw, _dense(bias, torch.float32, (F2,)), M, K, F, _dtype_code(X), act, h, ldh, z, ldz,
-                                             workspace.data_ptr(), workspace.nbytes, _stream(stream))
+    rc = (_marshal or _load_marshal()).gated_forward(X, W, bias, H, Z, act, workspace, _handle(stream))
     if rc:
         raise DpclipError("dpclip_gated_forward", rc)
 
 
 def dpclip_gated_backward(dH: torch.Tensor, Z: torch.Tensor, W: Optional[torch.Tensor], dZ: torch.Tensor, dX: Optional[torch.Tensor],
-                          act: int, workspace: torch.Tensor, stream=None) -> None:
+                          act: int, workspace: Optional[torch.Tensor], stream=None) -> None:
     """dZ (..., 2F), the signal of Layer(X, dZ), and dX (..., K) or None, from dH (..., F) and the Z of the forward pass."""
-    _on_device(dH, Z, W, dZ, dX, workspace)
-    dt = Z.dtype
-    z, ldz, M, F2 = _matrix(Z, dt, None, None)
-    F = F2 // 2
-    if F2 % 2:
-        raise ValueError("Z must have an even number of columns: gate, then up")
-    dh, lddh, _, _ = _matrix(dH, dt, M, F)
-    dz, lddz, _, _ = _matrix(dZ, dt, M, F2)
-    _writable(dZ.shape, dZ.stride())
-    w, ldw, K, dx, lddx = None, 0, 1, None, 0
-    if dX is not None:
-        if W is None:
-            raise ValueError("dX needs W")
-        w, ldw, _, K = _matrix(W, dt, F2, None)
-        dx, lddx, _, _ = _matrix(dX, dt, M, K)
-        _writable(dX.shape, dX.stride())
-    rc = load_library().dpclip_gated_backward(dh, lddh, z, ldz, w, ldw, M, K, F, _dtype_code(Z), act, dz, lddz, dx, lddx,
-                                              workspace.data_ptr(), workspace.nbytes, _stream(stream))
+    rc = (_marshal or _load_marshal()).gated_backward(dH, Z, W, dZ, dX, act, workspace, _handle(stream))
     if rc:
         raise DpclipError("dpclip_gated_backward", rc)

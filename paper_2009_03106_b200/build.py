@@ -10,6 +10,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(os.path.dirname(HERE), "include")
 LIB = os.path.join(HERE, "libdpclip.so")
+MARSHAL = os.path.join(HERE, "_marshal.so")                # Python module: arguments of the transformer-block calls
 LIB_DEBUG = os.path.join(HERE, "libdpclip_debug.so")       # -DDPCLIP_DEBUG: range-checked accesses
 
 NVCC_FLAGS = ["-std=c++17", "-O3", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo",
@@ -39,11 +40,41 @@ def _object_stale(obj: str, dep: str) -> bool:
     return any(not os.path.exists(n) or os.path.getmtime(n) > t for n in own)
 
 
+def _start_marshal(force: bool):
+    """Start compiling csrc/marshal.cpp, where it is newer than the module; None where there is nothing to do."""
+    src, dep = os.path.join(CSRC, "marshal.cpp"), os.path.join(INCLUDE, "dpclip.h")
+    if not force and os.path.exists(MARSHAL) and os.path.getmtime(MARSHAL) >= max(os.path.getmtime(src), os.path.getmtime(dep)):
+        return None
+    import sysconfig
+
+    import torch
+    root = os.path.dirname(torch.__file__)
+    tmp = MARSHAL + f".tmp{os.getpid()}"
+    cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden",
+           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", "-I" + INCLUDE, "-I" + sysconfig.get_paths()["include"],
+           "-isystem", os.path.join(root, "include"), "-isystem", os.path.join(root, "include", "torch", "csrc", "api", "include"),
+           "-isystem", os.path.join(os.environ.get("CUDA_HOME", "/usr/local/cuda"), "include"), src, "-L" + os.path.join(root, "lib"),
+           "-ltorch_python", "-ltorch", "-ltorch_cpu", "-lc10", "-lc10_cuda", "-o", tmp]
+    return cmd, tmp, subprocess.Popen(cmd)
+
+
+def _finish_marshal(started) -> None:
+    if started is None:
+        return
+    cmd, tmp, p = started
+    if p.wait() != 0:
+        raise subprocess.CalledProcessError(p.returncode, cmd)
+    os.replace(tmp, MARSHAL)
+
+
 def build(force: bool = False, verbose: bool = False, debug: bool = False) -> str:
-    """Compile every .cu under csrc/, each to an object of its own and all at once, and link one shared library.  Returns its path.
+    """Compile every .cu under csrc/, each to an object of its own and all at once, and link one shared library; and the Python module that
+    marshals arguments to it.  Returns the library's path.
     debug=True builds libdpclip_debug.so (range-checked accesses that set DPCLIP_ERR_RANGE and skip) beside it."""
     lib = LIB_DEBUG if debug else LIB
+    marshal = _start_marshal(force and not debug)
     if not force and not _stale(lib):
+        _finish_marshal(marshal)
         return lib
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
     objects = os.path.join(HERE, "build", "debug" if debug else "release")
@@ -65,6 +96,7 @@ def build(force: bool = False, verbose: bool = False, debug: bool = False) -> st
     tmp = lib + f".tmp{os.getpid()}"
     subprocess.check_call([nvcc] + NVCC_FLAGS + ["-shared"] + objs + ["-o", tmp])
     os.replace(tmp, lib)
+    _finish_marshal(marshal)
     return lib
 
 
