@@ -23,7 +23,7 @@ inline int clamp_int(long v, long lo, long hi) { return (int)(v < lo ? lo : v > 
 // ------------------------------------------------------------------------------------------------ relative position bias
 // thr[k], the smallest distance d of bucket exact + k: floor((n - exact) log(d / exact) / log(max / exact)) >= k, which is
 // d >= exact (max / exact)^(k / (n - exact)).  Borders that are whole numbers belong to the upper bucket; the powers are taken in extended
-// precision, where a border that is a whole number misses it by less than 1e-15 of itself.
+// precision, where a border that is a whole number misses it by less than 1e-16 of itself.
 bool fill_buckets(RbBuckets& r, const dpclip_relbias* c) {
     if (!c || c->n_buckets < 2 || c->n_buckets > RB_MAX_BUCKETS) return false;
     if (c->bidirectional && c->n_buckets % 2) return false;
@@ -36,11 +36,14 @@ bool fill_buckets(RbBuckets& r, const dpclip_relbias* c) {
     r.causal = c->causal != 0;
     if (r.exact < 1 || r.max_distance <= r.exact || r.max_distance > (1 << 24)) return false;
     const int m = r.n - r.exact;
-    const long double ratio = (long double)r.max_distance / r.exact;
-    for (int k = 0; k < m; ++k) {
-        const long double border = r.exact * powl(ratio, (long double)k / m), whole = roundl(border);
+    const long double step = powl((long double)r.max_distance / r.exact, 1.0L / m);
+    long double border = r.exact;                        // 128 steps at most: off by less than 1e-16 of itself at the last
+    for (int k = 0; k < m; ++k, border *= step) {
+        const long double whole = roundl(border);
         r.thr[k] = (int)(fabsl(border - whole) < 1e-12L * border ? whole : ceill(border));
     }
+    r.top = m > 1 ? 1 : 0;
+    while (m > 1 && 2 * r.top < m) r.top *= 2;
     for (int b = 0; b < r.n_buckets; ++b) {
         const int side = r.bidirectional && b >= r.n, c = b - (side ? r.n : 0);
         const int from = c < r.exact ? c : r.thr[c - r.exact];
@@ -67,7 +70,7 @@ RbTiles relbias_tiles(int B, int H, int Tq, int Tk, bool blocks8) {
     if (t.G > t.nqb) t.G = t.nqb;
     // long walks, as long as there are CTAs enough for every SM and 40 KB of shared memory hold the sums
     const int longest = blocks8 ? 32 : 128;
-    const long ctas = t.threads == RB_THREADS ? 6L * kNumSMs : 12L * kNumSMs;
+    const long ctas = t.threads == RB_THREADS ? 4L * kNumSMs : 12L * kNumSMs;
     t.nr = 1;
     auto fits = [&](int nr) { return (blocks8 ? rb_smem_floats<8>(t.KT, t.G, nr) : rb_smem_floats<1>(t.KT, t.G, nr)) * sizeof(float) <= 40 * 1024; };
     while (t.nr < longest && t.G * t.nr < t.nqb && fits(2 * t.nr) &&
@@ -166,7 +169,7 @@ int launch_qk_backward(QkParams& p, bool ring, cudaStream_t st) {
     constexpr int WARPS = QK_THREADS / 32;
     if constexpr (V > 1) {
         if (ring) {
-            constexpr int smem = WARPS * QK_BWD_STAGES * 4 * 512;      // 64 KB; the sums behind it need at most 16
+            const int smem = WARPS * QK_BWD_STAGES * 4 * 512 + (int)sizeof(float) * p.D;      // 48 KB and the gains; the sums, at most 16 KB, take the ring's place
             const auto kernel = p.interleaved ? qknorm_backward_ring_kernel<T, V, G, true> : qknorm_backward_ring_kernel<T, V, G, false>;
             if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return DPCLIP_ERR_CUDA;
             const dim3 grid(p.part[0].blocks * p.part[0].chunks + p.part[1].blocks * p.part[1].chunks, p.B);
@@ -175,7 +178,7 @@ int launch_qk_backward(QkParams& p, bool ring, cudaStream_t st) {
             return finish_launch();
         }
     }
-    constexpr int U = NCH <= 2 ? 2 : 1;
+    constexpr int U = V == 1 && NCH == 1 ? 4 : NCH <= 2 ? 2 : 1;
     const dim3 grid(p.part[0].chunks + p.part[1].chunks, p.B);
     qknorm_backward_kernel<T, V, NCH, G, U><<<grid, QK_THREADS, sizeof(float) * WARPS * p.D, st>>>(p);
     return finish_launch();
@@ -192,13 +195,13 @@ int launch_qk(QkParams& p, const QkShape& s, bool backward, bool ring, cudaStrea
 #undef DPCLIP_QK
 }
 
-// CTAs an example for `items` warp items of one part: about four CTAs an SM in all, at least sixteen items a CTA
-inline int qk_chunks(int B, long items) { return clamp_int(ceil_div(4L * kNumSMs, B), 1, items / 16 > 0 ? items / 16 : 1); }
+// CTAs an example for `items` of its `all` warp items: four CTAs an SM in all, one wave of them, and at least sixteen items a CTA
+inline int qk_chunks(int B, long items, long all) { return clamp_int(4L * kNumSMs * items / (all * B), 1, items / 16 > 0 ? items / 16 : 1); }
 // most partial sums an example any form of the kernels makes, for the workspace: one head a warp item without a ring; with one at most
 // H blocks of T / 64 chunks, and no more than its rule asks for
 inline long qk_most_sums(int B, int T, int H) {
     if (H <= 0) return 0;
-    const long plain = qk_chunks(B, (long)T * H), chunks = clamp_int(4L * kNumSMs / B, 1, T / 64 > 0 ? T / 64 : 1);
+    const long plain = qk_chunks(B, (long)T * H, (long)T * H), chunks = clamp_int(4L * kNumSMs / B, 1, T / 64 > 0 ? T / 64 : 1);
     const long ring = chunks * H < 4L * kNumSMs / B + H ? chunks * H : 4L * kNumSMs / B + H;
     return plain > ring ? plain : ring;
 }
@@ -320,7 +323,7 @@ int launch_gated_simt(GatedSimt& p, cudaStream_t st) {
 
 template <typename T, int V, int MT>
 int launch_gated_few(const GatedFew& p, cudaStream_t st) {
-    gated_few_kernel<T, V, MT><<<ceil_div(p.out.F, 4 * GF_ROWS), 128, 0, st>>>(p);
+    gated_few_kernel<T, V, MT><<<ceil_div(p.out.F, 4), 128, 0, st>>>(p);
     return finish_launch();
 }
 template <typename T, int V>
@@ -398,9 +401,8 @@ int dpclip_stored_clipped_grad(const float* grads, long ld, int B, int n, const 
     p.G = grads; p.ld = ld; p.B = B; p.n = n; p.clip = clip; p.g = g; p.noise_scale = sigma * C;
     p.k0 = (uint32_t)seed; p.k1 = (uint32_t)(seed >> 32); p.s0 = (uint32_t)stream_id; p.s1 = (uint32_t)(stream_id >> 32);
     cudaStream_t st = (cudaStream_t)stream;
-    if (B > 256) stored_grad_kernel<32><<<ceil_div(n, 32), 1024, 0, st>>>(p);
-    else stored_grad_kernel<8><<<ceil_div(n, 32), 256, 0, st>>>(p);
-    return finish_launch();
+    return B > 64 ? launch_after(stored_grad_kernel<32>, dim3(ceil_div(n, 32)), 1024, 0, st, p)
+                   : launch_after(stored_grad_kernel<8>, dim3(ceil_div(n, 32)), 256, 0, st, p);
 }
 
 int dpclip_relbias_bucket(const dpclip_relbias* config, long distance) {
@@ -521,7 +523,7 @@ int dpclip_qknorm_backward(const dpclip_heads* parts, int n_parts, int B, int T,
             q.chunks = clamp_int(4L * kNumSMs / ((long)B * (p.part[0].blocks + p.part[1].blocks)), 1, T / 64 > 0 ? T / 64 : 1);
             sums[k] = (size_t)q.blocks * q.chunks;
         } else {
-            q.chunks = qk_chunks(B, (long)T * q.blocks);
+            q.chunks = qk_chunks(B, (long)T * q.blocks, (long)T * (p.part[0].blocks + p.part[1].blocks));
             sums[k] = q.chunks;
         }
     }

@@ -241,6 +241,7 @@ gated_simt_kernel(const __grid_constant__ GatedSimt p) {
             else bs[b][(tid >> 7) + 2 * i][tid & 127] = rb[i];
         }
     };
+    griddep_launch_dependents();
     // thread's rows: ty * 4 + r and 64 + ty * 4 + r (BM = 128), or ty * 2 + r (BM = 32); columns: tx * 4 + c and 64 + tx * 4 + c, in pairs
     f32x2 acc2[RM][4];
 #pragma unroll
@@ -316,67 +317,83 @@ struct GatedFew {
     int K;
     GatedOut out;
 };
-template <typename T, int V> __device__ __forceinline__ void gated_vec(const T* p, float (&x)[V]) {
-    if constexpr (V == 1) x[0] = to_f32(*p);
-    else if constexpr (V == 4) {
-        const float4 v = __ldg(reinterpret_cast<const float4*>(p));
-        x[0] = v.x; x[1] = v.y; x[2] = v.z; x[3] = v.w;
-    } else {
-        const uint4 v = __ldg(reinterpret_cast<const uint4*>(p));
-        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+template <typename T, int V> struct GatedRaw { uint4 v; };
+template <typename T> struct GatedRaw<T, 1> { T v; };
+template <typename T, int V> __device__ __forceinline__ void gated_load(const T* p, GatedRaw<T, V>& r) {
+    if constexpr (V == 1) r.v = *p;
+    else r.v = __ldg(reinterpret_cast<const uint4*>(p));
+}
+template <typename T, int V> __device__ __forceinline__ void gated_vec(const GatedRaw<T, V>& r, float (&x)[V]) {
+    if constexpr (V == 1) x[0] = to_f32(r.v);
+    else {
+        const uint32_t w[4] = {r.v.x, r.v.y, r.v.z, r.v.w};
 #pragma unroll
-        for (int k = 0; k < 4; ++k) { x[2 * k] = __uint_as_float(w[k] << 16); x[2 * k + 1] = __uint_as_float(w[k] & 0xFFFF0000u); }
+        for (int k = 0; k < 4; ++k) {
+            if constexpr (V == 8) { x[2 * k] = __uint_as_float(w[k] << 16); x[2 * k + 1] = __uint_as_float(w[k] & 0xFFFF0000u); }
+            else x[k] = __uint_as_float(w[k]);
+        }
     }
 }
-constexpr int GF_ROWS = 1;               // gate rows of W a warp, and as many up rows
+// A warp: one gate row of W and its up row.  The lanes take 16 bytes each of a row, and the loads of four rounds go out before the first is
+// used: a thousand columns are then one round trip to memory.
+constexpr int GF_ROUNDS = 4;
 template <typename T, int V, int MT>
 __global__ void __launch_bounds__(128)
 gated_few_kernel(const __grid_constant__ GatedFew p) {
-    const int lane = threadIdx.x & 31, f0 = (blockIdx.x * 4 + (threadIdx.x >> 5)) * GF_ROWS;
+    const int lane = threadIdx.x & 31, f = blockIdx.x * 4 + (threadIdx.x >> 5);
     const int F = p.out.F, M = p.out.M;
-    if (f0 >= F) return;
-    const T* row[2 * GF_ROWS];
+    if (f >= F) return;
+    const T* const gate = static_cast<const T*>(p.w) + (long)f * p.ldw;
+    const T* const up = static_cast<const T*>(p.w) + ((long)F + f) * p.ldw;
+    const T* x[MT];
 #pragma unroll
-    for (int r = 0; r < GF_ROWS; ++r) {
-        const int f = min(f0 + r, F - 1);
-        row[r] = static_cast<const T*>(p.w) + (long)f * p.ldw;
-        row[GF_ROWS + r] = static_cast<const T*>(p.w) + (long)(F + f) * p.ldw;
-    }
-    float acc[2 * GF_ROWS][MT];
+    for (int m = 0; m < MT; ++m) x[m] = static_cast<const T*>(p.x) + (long)min(m, M - 1) * p.ldx;     // rows behind the last: sums nobody writes
+    float g[MT], u[MT];
 #pragma unroll
-    for (int r = 0; r < 2 * GF_ROWS; ++r)
+    for (int m = 0; m < MT; ++m) { g[m] = 0.f; u[m] = 0.f; }
+    int k = lane * V;
+    for (; k + (GF_ROUNDS - 1) * 32 * V < p.K; k += GF_ROUNDS * 32 * V) {
+        GatedRaw<T, V> a[GF_ROUNDS], b[GF_ROUNDS];
 #pragma unroll
-        for (int m = 0; m < MT; ++m) acc[r][m] = 0.f;
-#pragma unroll 4
-    for (int k = lane * V; k < p.K; k += 32 * V) {
-        float w[2 * GF_ROWS][V];
+        for (int i = 0; i < GF_ROUNDS; ++i) { gated_load<T, V>(gate + k + i * 32 * V, a[i]); gated_load<T, V>(up + k + i * 32 * V, b[i]); }
 #pragma unroll
-        for (int r = 0; r < 2 * GF_ROWS; ++r) gated_vec<T, V>(row[r] + k, w[r]);
+        for (int i = 0; i < GF_ROUNDS; ++i) {
+            float wa[V], wb[V];
+            gated_vec<T, V>(a[i], wa);
+            gated_vec<T, V>(b[i], wb);
 #pragma unroll
-        for (int m = 0; m < MT; ++m) {
-            if (m < M) {
-                float x[V];
-                gated_vec<T, V>(static_cast<const T*>(p.x) + (long)m * p.ldx + k, x);
+            for (int m = 0; m < MT; ++m) {
+                GatedRaw<T, V> r;
+                float xv[V];
+                gated_load<T, V>(x[m] + k + i * 32 * V, r);
+                gated_vec<T, V>(r, xv);
 #pragma unroll
-                for (int r = 0; r < 2 * GF_ROWS; ++r)
-#pragma unroll
-                    for (int v = 0; v < V; ++v) acc[r][m] = fmaf(w[r][v], x[v], acc[r][m]);
+                for (int v = 0; v < V; ++v) { g[m] = fmaf(wa[v], xv[v], g[m]); u[m] = fmaf(wb[v], xv[v], u[m]); }
             }
         }
     }
+    for (; k < p.K; k += 32 * V) {
+        GatedRaw<T, V> a, b, r;
+        float wa[V], wb[V], xv[V];
+        gated_load<T, V>(gate + k, a);
+        gated_load<T, V>(up + k, b);
+        gated_vec<T, V>(a, wa);
+        gated_vec<T, V>(b, wb);
 #pragma unroll
-    for (int r = 0; r < 2 * GF_ROWS; ++r)
+        for (int m = 0; m < MT; ++m) {
+            gated_load<T, V>(x[m] + k, r);
+            gated_vec<T, V>(r, xv);
 #pragma unroll
-        for (int m = 0; m < MT; ++m) acc[r][m] = warp_sum(acc[r][m]);
-    // lane (m, r) writes; a choice among registers, not an index into them
-    float g = 0.f, u = 0.f;
+            for (int v = 0; v < V; ++v) { g[m] = fmaf(wa[v], xv[v], g[m]); u[m] = fmaf(wb[v], xv[v], u[m]); }
+        }
+    }
+    float mine_g = 0.f, mine_u = 0.f;
 #pragma unroll
-    for (int r = 0; r < GF_ROWS; ++r)
-#pragma unroll
-        for (int m = 0; m < MT; ++m)
-            if (lane == m * GF_ROWS + r) { g = acc[r][m]; u = acc[GF_ROWS + r][m]; }
-    const int m = lane / GF_ROWS, f = f0 + lane % GF_ROWS;
-    if (m < M && m < MT && f < F) gated_end<T>(p.out, m, f, g, u);
+    for (int m = 0; m < MT; ++m) {
+        const float a = warp_sum(g[m]), b = warp_sum(u[m]);
+        if (lane == m) { mine_g = a; mine_u = b; }
+    }
+    if (lane < M && lane < MT) gated_end<T>(p.out, lane, f, mine_g, mine_u);
 }
 
 // ------------------------------------------------------------------------------------------------ tensor cores

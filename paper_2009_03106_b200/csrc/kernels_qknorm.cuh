@@ -132,6 +132,19 @@ template <int V> __device__ __forceinline__ QkVec<V> qk_params(const float* p) {
     return x;
 }
 
+template <int V> __device__ __forceinline__ QkVec<V> qk_shared(const float* p) {
+    QkVec<V> x;
+#pragma unroll
+    for (int u = 0; u < V / 4; ++u) {
+        float4 f;                        // volatile: a value kept in registers is what this is to avoid
+        asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(f.x), "=f"(f.y), "=f"(f.z), "=f"(f.w)
+                     : "r"((uint32_t)__cvta_generic_to_shared(p + 4 * u)));
+        x.v[2 * u] = make_f32x2(f.x, f.y);
+        x.v[2 * u + 1] = make_f32x2(f.z, f.w);
+    }
+    return x;
+}
+
 // Where the V + V elements of chunk c lie: two runs of V, [a0, a0 + V) and [a1, a1 + V); angles [rot0, rot0 + V) where turned.
 template <int V>
 struct QkChunk {
@@ -275,12 +288,22 @@ qknorm_backward_kernel(const __grid_constant__ QkParams p) {
         if (y.gain && c[n].there) gain0[n] = qk_params<V>(y.gain + c[n].a0);
         if (y.gain && c[n].second) gain1[n] = qk_params<V>(y.gain + c[n].a1);
     }
+    griddep_launch_dependents();
     const float inv_d = 1.f / (float)p.D;
     const T* const x0 = static_cast<const T*>(y.x) + (long)b * y.xb;
     const T* const d0 = static_cast<const T*>(y.dy) + (long)b * y.yb;
     T* const o0 = static_cast<T*>(y.y) + (long)b * y.ob;
     const uint32_t stride = (uint32_t)y.chunks * WARPS;
-    for (uint32_t item0 = (uint32_t)chunk * WARPS + warp; item0 < items; item0 += stride * U) {
+    // positions are loaded a round ahead: the loads of a row wait for them
+    auto position = [&](uint32_t item) {
+        const int t = (int)(item / (uint32_t)y.blocks);
+        return item < items ? qk_position(p, (uint32_t)b * p.T + t, t) : -1;
+    };
+    long ahead[U];
+    const uint32_t item1 = (uint32_t)chunk * WARPS + warp;
+#pragma unroll
+    for (int k = 0; k < U; ++k) ahead[k] = position(item1 + k * stride);
+    for (uint32_t item0 = item1; item0 < items; item0 += stride * U) {
         QkRaw<T, V> xl[U][NCH], xh[U][NCH], yl[U][NCH], yh[U][NCH];
         long pos[U];
         T* out[U];
@@ -290,7 +313,8 @@ qknorm_backward_kernel(const __grid_constant__ QkParams p) {
             const int t = (int)(item / (uint32_t)y.blocks);
             const int h = (int)(item - (uint32_t)t * y.blocks) * NG + grp;
             const bool on = item < items && h < y.H;
-            pos[k] = on ? qk_position(p, (uint32_t)b * p.T + t, t) : -1;
+            pos[k] = on ? ahead[k] : -1;
+            ahead[k] = position(item + stride * U);
             out[k] = on ? o0 + (long)t * y.ot + (long)h * y.oh : nullptr;
             const T* x = x0 + (long)t * y.xt + (long)h * y.xh;
             const T* d = d0 + (long)t * y.yt + (long)h * y.yh;
@@ -453,7 +477,7 @@ template <int V> struct QkAngles {
     }
 };
 
-constexpr int QK_FWD_STAGES = 6, QK_BWD_STAGES = 4;
+constexpr int QK_FWD_STAGES = 6, QK_BWD_STAGES = 3;      // backward: 126 us with three, 134 with four, 136 with six (453 MB)
 
 // A warp's walk is over the tokens of the whole batch: blockIdx.x * WARPS + warp, step gridDim.x * WARPS.
 template <typename T, int V, int G, bool INTER>
@@ -538,7 +562,7 @@ template <typename T, int V, int G, bool INTER>
 __global__ void __launch_bounds__(QK_THREADS, 2)
 qknorm_backward_ring_kernel(const __grid_constant__ QkParams p) {
     constexpr int NG = 32 / G, WARPS = QK_THREADS / 32, ST = QK_BWD_STAGES;
-    extern __shared__ __align__(16) uint8_t qk_ring[];   // [WARPS][ST][4][32 * 16], then [WARPS][D] floats over it
+    extern __shared__ __align__(16) uint8_t qk_ring[];   // [WARPS][ST][4][32 * 16], later [WARPS][D] floats over it; [D] gains
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, gl = lane % G, grp = lane / G;
     const int units0 = p.part[0].blocks * p.part[0].chunks;
     const int which = (int)blockIdx.x >= units0;
@@ -554,14 +578,20 @@ qknorm_backward_ring_kernel(const __grid_constant__ QkParams p) {
     char* out = reinterpret_cast<char*>(static_cast<T*>(y.y) + (long)b * y.ob + (long)first * y.ot + (mine ? (long)h * y.oh + c.a0 : 0));
     const long x_inc = (long)step * y.xt * (long)sizeof(T), d_inc = (long)step * y.yt * (long)sizeof(T), o_inc = (long)step * y.ot * (long)sizeof(T);
     const int far = mine ? (c.a1 - c.a0) * (int)sizeof(T) : 0;
-    QkVec<V> gain0 = qk_fill<V>(1.f), gain1 = gain0, acc0 = qk_fill<V>(0.f), acc1 = acc0;
-    if (y.gain && c.there) { gain0 = qk_params<V>(y.gain + c.a0); gain1 = qk_params<V>(y.gain + c.a1); }
+    QkVec<V> acc0 = qk_fill<V>(0.f), acc1 = acc0;
+    // the gains stay in shared memory: the sums, a row of each input and the angles fill the registers
+    float* const gains = reinterpret_cast<float*>(qk_ring + WARPS * ST * 4 * 512);
+    for (int i = threadIdx.x; i < p.D; i += QK_THREADS) gains[i] = y.gain ? y.gain[i] : 1.f;
+    __syncthreads();
+    const float* const gain_a = gains + (c.there ? c.a0 : 0);
+    const float* const gain_b = gains + (c.there ? c.a1 : 0);
     const float inv_d = 1.f / (float)p.D;
     const uint32_t slot0 = (uint32_t)__cvta_generic_to_shared(qk_ring + warp * (ST * 4 * 512) + lane * 16);
     const char* const table = reinterpret_cast<const char*>(p.table + c.rot0);
     const uint32_t pitch = p.rot * 4, half = p.rot * 2;
     const int n_pos = (int)p.n_pos;
 
+    griddep_launch_dependents();
     QkPositions where(p.pos ? p.pos + (long)b * p.T : nullptr, first, step, T_);
     uint32_t t_load = first;
     int pos[ST];
@@ -580,13 +610,13 @@ qknorm_backward_ring_kernel(const __grid_constant__ QkParams p) {
     };
 #pragma unroll
     for (int s = 0; s < ST - 1; ++s) issue(s);
-    QkAngles<V> ahead;
-    ahead.c = qk_fill<V>(1.f); ahead.s = qk_fill<V>(0.f);
-    ahead.load(table, pos[0], pitch, half, c.turned);
     for (uint32_t t = first; t < T_;) {
 #pragma unroll
         for (int s = 0; s < ST; ++s) {
             if (t >= T_) break;
+            QkAngles<V> turn;
+            turn.c = qk_fill<V>(1.f); turn.s = qk_fill<V>(0.f);
+            turn.load(table, pos[s], pitch, half, c.turned);
             qk_copy_wait<ST - 2>();
             QkRaw<T, V> xl, xr, yl, yr;
             yl.v = qk_lds16(slot0 + (s * 4 + 2) * 512);
@@ -596,14 +626,13 @@ qknorm_backward_ring_kernel(const __grid_constant__ QkParams p) {
             const int at = pos[s];
             issue((s + ST - 1) % ST);
             QkVec<V> ga = qk_f32<T, V>(yl), gb = qk_f32<T, V>(yr);
-            if (c.turned) qk_turn2<V, INTER, true>(ga, gb, ahead.c, ahead.s);
-            ahead.load(table, pos[(s + 1) % ST], pitch, half, c.turned);
+            if (c.turned) qk_turn2<V, INTER, true>(ga, gb, turn.c, turn.s);
             const QkVec<V> xa = qk_f32<T, V>(xl), xb = qk_f32<T, V>(xr);
             f32x2 ss = make_f32x2(0.f, 0.f), dots = make_f32x2(0.f, 0.f);
             qk_dot<V>(ss, xa, xa);
             qk_dot<V>(ss, xb, xb);
-            qk_dot<V>(dots, qk_mul<V>(ga, gain0), xa);
-            qk_dot<V>(dots, qk_mul<V>(gb, gain1), xb);
+            qk_dot<V>(dots, qk_mul<V>(ga, qk_shared<V>(gain_a)), xa);
+            qk_dot<V>(dots, qk_mul<V>(gb, qk_shared<V>(gain_b)), xb);
             const float sum = qk_group_sum<G>(sum_f32x2(ss)), dot = qk_group_sum<G>(sum_f32x2(dots));
             const float r = at >= 0 ? rsqrtf(fmaf(sum, inv_d, p.eps)) : 0.f;
             const QkVec<V> rr = qk_fill<V>(r), m = qk_fill<V>(-(dot * inv_d * r * r * r));   // m: what dx has of x
@@ -612,8 +641,8 @@ qknorm_backward_ring_kernel(const __grid_constant__ QkParams p) {
             acc0 = qk_fma<V>(ga, xa, acc0);
             acc1 = qk_fma<V>(gb, xb, acc1);
             if (mine) {
-                qk_store<T, V>(reinterpret_cast<T*>(out), qk_fma<V>(m, xa, qk_mul<V>(ga, gain0)));
-                qk_store<T, V>(reinterpret_cast<T*>(out + far), qk_fma<V>(m, xb, qk_mul<V>(gb, gain1)));
+                qk_store<T, V>(reinterpret_cast<T*>(out), qk_fma<V>(m, xa, qk_mul<V>(ga, qk_shared<V>(gain_a))));
+                qk_store<T, V>(reinterpret_cast<T*>(out + far), qk_fma<V>(m, xb, qk_mul<V>(gb, qk_shared<V>(gain_b))));
             }
             t += step; out += o_inc;
         }
@@ -649,6 +678,7 @@ __global__ void __launch_bounds__(QK_THREADS)
 qknorm_finish_kernel(const __grid_constant__ QkFinish p) {
     __shared__ float red[32];
     griddep_wait();
+    griddep_launch_dependents();
     const int i = blockIdx.x, which = blockIdx.y, chunks = p.chunks[which];
     float total = 0.f;
     for (int d = threadIdx.x; d < p.D; d += QK_THREADS) {

@@ -29,6 +29,7 @@ constexpr int RB_FAR = 1 << 30;
 // logarithmic scale; thr[k] is the smallest distance of bucket exact + k.
 struct RbBuckets {
     int n_buckets, n, exact, max_distance, bidirectional, causal;
+    int top;                                         // the largest power of two below n - exact, or 0
     int thr[RB_MAX_BUCKETS];
     int lo[RB_MAX_BUCKETS], hi[RB_MAX_BUCKETS];      // the distances of every bucket, empty where lo > hi; RB_FAR: no end
 };
@@ -91,11 +92,25 @@ relbias_forward_kernel(const __grid_constant__ RbForward p) {
 #pragma unroll
                 for (int j = 0; j < 2 * E - 1; ++j) v[j] = x;
             } else {
-#pragma unroll 1
-                for (int j = 0; j < 2 * E - 1; ++j) {
-                    const float x = value(first + j);
+                // the searches of all distances side by side: one after the other they are a chain of round trips
+                int d[2 * E - 1], k[2 * E - 1];
 #pragma unroll
-                    for (int i = 0; i < 2 * E - 1; ++i) if (i == j) v[i] = x;
+                for (int j = 0; j < 2 * E - 1; ++j) {
+                    const long rel = first + j;
+                    const int x = (int)(rel > p.r.max_distance ? p.r.max_distance : rel < -(long)p.r.max_distance ? -p.r.max_distance : rel);
+                    d[j] = p.r.bidirectional ? abs(x) : max(-x, 0);
+                    k[j] = 0;
+                }
+                for (int s = p.r.top; s > 0; s >>= 1) {
+#pragma unroll
+                    for (int j = 0; j < 2 * E - 1; ++j)
+                        if (k[j] + s < p.r.n - p.r.exact && p.r.thr[k[j] + s] <= d[j]) k[j] += s;
+                }
+#pragma unroll
+                for (int j = 0; j < 2 * E - 1; ++j) {
+                    const long rel = first + j;
+                    const int b = (p.r.bidirectional && rel > 0 ? p.r.n : 0) + (d[j] < p.r.exact ? d[j] : p.r.exact + k[j]);
+                    v[j] = p.r.causal && rel > 0 ? __int_as_float(0xFF800000) : __ldg(column + (long)b * p.ldt);
                 }
             }
         } else {
@@ -287,6 +302,7 @@ template <typename T, int E, int THREADS>
 __global__ void __launch_bounds__(THREADS, 512 / THREADS)
 relbias_grad_kernel(const __grid_constant__ RbGrad p) {
     extern __shared__ __align__(16) float rb_smem[];
+    griddep_launch_dependents();
     const int tid = threadIdx.x;
     const int tiles = p.qtiles * p.ktiles;
     const long bh = (long)blockIdx.x / tiles;
@@ -388,6 +404,7 @@ relbias_finish_kernel(const float* __restrict__ part, int H, int tiles, int n_bu
                       float* __restrict__ grads, float* __restrict__ sq) {
     __shared__ float red[32];
     griddep_wait();
+    griddep_launch_dependents();
     const int i = blockIdx.x, n = n_buckets * H;
     const int lane = threadIdx.x & (lanes - 1), per = RB_FINISH_THREADS / lanes;
     float* const g = grads + (size_t)i * n;

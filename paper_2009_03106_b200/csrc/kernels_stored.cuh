@@ -2,8 +2,8 @@
 // norm kernel has left in memory (a few hundred numbers an example).
 //
 // CTA = 32 columns; its warps deal the examples among them with eight loads in flight, the warps' sums are added in order.  The bytes
-// are few (128 examples of 512 numbers: 256 KB), so what bounds it is the round trip of the loads.  32 warps where there are more than 256
-// examples.
+// are few (128 examples of 512 numbers: 256 KB), so what bounds it is the round trip of the loads.  32 warps where eight would go
+// round more than once.
 #pragma once
 #include "philox.cuh"
 
@@ -22,6 +22,8 @@ stored_grad_kernel(const __grid_constant__ StoredParams p) {
     __shared__ float part[WARPS][32];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int c = blockIdx.x * 32 + lane;
+    griddep_wait();
+    griddep_launch_dependents();
     float acc = 0.f;
     if (c < p.n) {
         for (int i = warp; i < p.B; i += WARPS * UNR) {
