@@ -117,9 +117,11 @@ bool qk_shape(QkShape& s, int D, int rot, bool vec, dpclip_dtype dtype) {
         while (s.G < D / (2 * v)) s.G *= 2;
         return true;
     }
-    s.V = 1; s.G = 32;
+    // four pairs a lane where that fills the lanes of a head: shorter sums across lanes and several heads a warp
+    s.V = 1;
     const int pairs = (D + 1) / 2;
-    s.NCH = pairs <= 32 ? 1 : pairs <= 64 ? 2 : pairs <= 128 ? 4 : 8;
+    s.NCH = pairs <= 128 ? 4 : 8;
+    s.G = pairs <= 32 ? 8 : pairs <= 64 ? 16 : 32;
     return pairs <= 256;
 }
 
@@ -178,16 +180,19 @@ int launch_qk_backward(QkParams& p, bool ring, cudaStream_t st) {
             return finish_launch();
         }
     }
-    constexpr int U = V == 1 && NCH == 1 ? 4 : NCH <= 2 ? 2 : 1;
-    const dim3 grid(p.part[0].chunks + p.part[1].chunks, p.B);
-    qknorm_backward_kernel<T, V, NCH, G, U><<<grid, QK_THREADS, sizeof(float) * WARPS * p.D, st>>>(p);
+    const int warps = p.T < WARPS ? p.T : WARPS;
+    const dim3 grid(p.part[0].blocks * p.part[0].chunks + p.part[1].blocks * p.part[1].chunks, p.B);
+    qknorm_backward_kernel<T, V, NCH, G><<<grid, 32 * warps, sizeof(float) * warps * p.D, st>>>(p);
     return finish_launch();
 }
 template <typename T>
 int launch_qk(QkParams& p, const QkShape& s, bool backward, bool ring, cudaStream_t st) {
     constexpr int VV = sizeof(T) == 4 ? 4 : 8;
 #define DPCLIP_QK(V, NCH, G) return backward ? launch_qk_backward<T, V, NCH, G>(p, ring, st) : launch_qk_forward<T, V, NCH, G>(p, st)
-    if (s.V == 1) switch (s.NCH) { case 1: DPCLIP_QK(1, 1, 32); case 2: DPCLIP_QK(1, 2, 32); case 4: DPCLIP_QK(1, 4, 32); default: DPCLIP_QK(1, 8, 32); }
+    if (s.V == 1) {
+        if (s.NCH == 8) DPCLIP_QK(1, 8, 32);
+        switch (s.G) { case 8: DPCLIP_QK(1, 4, 8); case 16: DPCLIP_QK(1, 4, 16); default: DPCLIP_QK(1, 4, 32); }
+    }
     switch (s.G) {
         case 1: DPCLIP_QK(VV, 1, 1); case 2: DPCLIP_QK(VV, 1, 2); case 4: DPCLIP_QK(VV, 1, 4);
         case 8: DPCLIP_QK(VV, 1, 8); case 16: DPCLIP_QK(VV, 1, 16); default: DPCLIP_QK(VV, 1, 32);
@@ -195,15 +200,17 @@ int launch_qk(QkParams& p, const QkShape& s, bool backward, bool ring, cudaStrea
 #undef DPCLIP_QK
 }
 
-// CTAs an example for `items` of its `all` warp items: four CTAs an SM in all, one wave of them, and at least sixteen items a CTA
-inline int qk_chunks(int B, long items, long all) { return clamp_int(4L * kNumSMs * items / (all * B), 1, items / 16 > 0 ? items / 16 : 1); }
-// most partial sums an example any form of the kernels makes, for the workspace: one head a warp item without a ring; with one at most
-// H blocks of T / 64 chunks, and no more than its rule asks for
+// Chunks of positions a block of heads is cut into: about four CTAs an SM in all (two where a ring of copies is kept), at least `least`
+// positions each.
+inline int qk_chunks(int B, int T, int blocks, bool ring) {
+    const int least = ring ? 64 : 16;
+    return clamp_int(4L * kNumSMs / ((long)B * blocks), 1, T / least > 0 ? T / least : 1);
+}
+// most partial sums an example any form of the kernels makes, for the workspace
 inline long qk_most_sums(int B, int T, int H) {
     if (H <= 0) return 0;
-    const long plain = qk_chunks(B, (long)T * H, (long)T * H), chunks = clamp_int(4L * kNumSMs / B, 1, T / 64 > 0 ? T / 64 : 1);
-    const long ring = chunks * H < 4L * kNumSMs / B + H ? chunks * H : 4L * kNumSMs / B + H;
-    return plain > ring ? plain : ring;
+    const long chunks = clamp_int(4L * kNumSMs / B, 1, T / 16 > 0 ? T / 16 : 1);
+    return chunks * H < 4L * kNumSMs / B + H ? chunks * H : 4L * kNumSMs / B + H;
 }
 
 int qk_check(const dpclip_heads* parts, int n_parts, int B, int T, int D, int rot_dim, const float* table, long n_pos,
@@ -211,7 +218,7 @@ int qk_check(const dpclip_heads* parts, int n_parts, int B, int T, int D, int ro
     if (!parts || n_parts < 1 || n_parts > 2 || B <= 0 || T <= 0 || D <= 0 || !dtype_known(dtype)) return DPCLIP_ERR_INVALID_ARG;
     if (rot_dim < 0 || rot_dim > D || rot_dim % 2 || !(eps >= 0.f) || n_pos <= 0) return DPCLIP_ERR_INVALID_ARG;
     if ((rot_dim > 0 && !table) || (!positions && pos0 < 0)) return DPCLIP_ERR_INVALID_ARG;
-    if ((long)B * T > 0x7FFFFFFFL - 4096 || D > 512 || (backward && B > 65535)) return DPCLIP_ERR_UNSUPPORTED;
+    if ((long)B * T > 0x7FFF0000L || D > 512 || (backward && B > 65535)) return DPCLIP_ERR_UNSUPPORTED;
     const size_t es = elt_size(dtype);
     for (int k = 0; k < n_parts; ++k) {
         const dpclip_heads& h = parts[k];
@@ -517,15 +524,8 @@ int dpclip_qknorm_backward(const dpclip_heads* parts, int n_parts, int B, int T,
     }
     const bool ring = qk_ring_backward(s, B, T, p.part);
     for (int k = 0; k < n_parts; ++k) {
-        QkPart& q = p.part[k];
-        if (ring) {
-            // about two waves of two CTAs an SM, at least 64 positions a CTA
-            q.chunks = clamp_int(4L * kNumSMs / ((long)B * (p.part[0].blocks + p.part[1].blocks)), 1, T / 64 > 0 ? T / 64 : 1);
-            sums[k] = (size_t)q.blocks * q.chunks;
-        } else {
-            q.chunks = qk_chunks(B, (long)T * q.blocks, (long)T * (p.part[0].blocks + p.part[1].blocks));
-            sums[k] = q.chunks;
-        }
+        p.part[k].chunks = qk_chunks(B, T, p.part[0].blocks + p.part[1].blocks, ring);
+        sums[k] = (size_t)p.part[k].blocks * p.part[k].chunks;
     }
     if (!workspace || !is_aligned(workspace, 16) || workspace_bytes < kHeaderBytes + sizeof(float) * B * (sums[0] + sums[1]) * D)
         return DPCLIP_ERR_WORKSPACE;

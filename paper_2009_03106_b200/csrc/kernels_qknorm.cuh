@@ -264,20 +264,21 @@ qknorm_forward_kernel(const __grid_constant__ QkParams p) {
     }
 }
 
-// CTA = a chunk of one example's (token, head block) items of one part; its threads keep the gain's gradient of their elements in
-// registers over the chunk.
-template <typename T, int V, int NCH, int G, int U>
+// CTA = chunk of the positions of one example and one block of heads: blockIdx.x = (queries' blocks x chunks, then the keys'), blockIdx.y =
+// example; its warps (up to eight, no more than there are positions) walk positions chunk * warps + warp, step chunks * warps, the next
+// position's loads under way while one is worked on.  The threads keep the gain's gradient of their elements in registers.
+template <typename T, int V, int NCH, int G>
 __global__ void __launch_bounds__(QK_THREADS, NCH * V <= 8 ? 2 : 1)
 qknorm_backward_kernel(const __grid_constant__ QkParams p) {
-    constexpr int NG = 32 / G, WARPS = QK_THREADS / 32;
-    extern __shared__ float qk_smem[];                   // [WARPS][D]
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, gl = lane % G, grp = lane / G;
-    int chunk = blockIdx.x;
-    const int which = chunk >= p.part[0].chunks;
-    if (which) chunk -= p.part[0].chunks;
+    constexpr int NG = 32 / G;
+    extern __shared__ float qk_smem[];                   // [warps][D]
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5, gl = lane % G, grp = lane / G;
+    const int units0 = p.part[0].blocks * p.part[0].chunks;
+    const int which = (int)blockIdx.x >= units0;
     const QkPart& y = p.part[which];
-    const int b = blockIdx.y;
-    const uint32_t items = (uint32_t)p.T * y.blocks;     // of one example
+    const int unit = (int)blockIdx.x - (which ? units0 : 0), block = unit / y.chunks, chunk = unit - block * y.chunks;
+    const int h = block * NG + grp, b = blockIdx.y;
+    const bool head = h < y.H;
     QkChunk<V> c[NCH];
     QkVec<V> gain0[NCH], gain1[NCH], acc0[NCH], acc1[NCH];
 #pragma unroll
@@ -290,73 +291,61 @@ qknorm_backward_kernel(const __grid_constant__ QkParams p) {
     }
     griddep_launch_dependents();
     const float inv_d = 1.f / (float)p.D;
-    const T* const x0 = static_cast<const T*>(y.x) + (long)b * y.xb;
-    const T* const d0 = static_cast<const T*>(y.dy) + (long)b * y.yb;
-    T* const o0 = static_cast<T*>(y.y) + (long)b * y.ob;
-    const uint32_t stride = (uint32_t)y.chunks * WARPS;
-    // positions are loaded a round ahead: the loads of a row wait for them
-    auto position = [&](uint32_t item) {
-        const int t = (int)(item / (uint32_t)y.blocks);
-        return item < items ? qk_position(p, (uint32_t)b * p.T + t, t) : -1;
+    const int first = chunk * warps + warp, step = y.chunks * warps;
+    const T* x = static_cast<const T*>(y.x) + (long)b * y.xb + (long)first * y.xt + (head ? (long)h * y.xh : 0);
+    const T* d = static_cast<const T*>(y.dy) + (long)b * y.yb + (long)first * y.yt + (head ? (long)h * y.yh : 0);
+    T* out = static_cast<T*>(y.y) + (long)b * y.ob + (long)first * y.ot + (head ? (long)h * y.oh : 0);
+    const long x_inc = (long)step * y.xt, d_inc = (long)step * y.yt, o_inc = (long)step * y.ot;
+    auto position = [&](int t) { return t < p.T ? qk_position(p, (uint32_t)b * p.T + t, t) : -1; };
+    QkRaw<T, V> xl[NCH], xr[NCH], yl[NCH], yr[NCH];
+    auto load = [&](long at) {                           // a padding row counts as zeros, whatever it holds
+        const bool live = head && at >= 0;
+#pragma unroll
+        for (int n = 0; n < NCH; ++n) {
+            qk_zero(xl[n]); qk_zero(xr[n]); qk_zero(yl[n]); qk_zero(yr[n]);
+            if (live && c[n].there) { qk_load(x + c[n].a0, xl[n]); qk_load(d + c[n].a0, yl[n]); }
+            if (live && c[n].second) { qk_load(x + c[n].a1, xr[n]); qk_load(d + c[n].a1, yr[n]); }
+        }
+        x += x_inc; d += d_inc;
     };
-    long ahead[U];
-    const uint32_t item1 = (uint32_t)chunk * WARPS + warp;
+    long at = position(first), ahead = position(first + step);
+    load(at);
+    for (int t = first; t < p.T; t += step) {
+        QkVec<V> xa[NCH], xb[NCH], ga[NCH], gb[NCH];
 #pragma unroll
-    for (int k = 0; k < U; ++k) ahead[k] = position(item1 + k * stride);
-    for (uint32_t item0 = item1; item0 < items; item0 += stride * U) {
-        QkRaw<T, V> xl[U][NCH], xh[U][NCH], yl[U][NCH], yh[U][NCH];
-        long pos[U];
-        T* out[U];
-#pragma unroll
-        for (int k = 0; k < U; ++k) {
-            const uint32_t item = item0 + k * stride;
-            const int t = (int)(item / (uint32_t)y.blocks);
-            const int h = (int)(item - (uint32_t)t * y.blocks) * NG + grp;
-            const bool on = item < items && h < y.H;
-            pos[k] = on ? ahead[k] : -1;
-            ahead[k] = position(item + stride * U);
-            out[k] = on ? o0 + (long)t * y.ot + (long)h * y.oh : nullptr;
-            const T* x = x0 + (long)t * y.xt + (long)h * y.xh;
-            const T* d = d0 + (long)t * y.yt + (long)h * y.yh;
-            const bool live = pos[k] >= 0;               // a padding row counts as zeros, whatever it holds
-#pragma unroll
-            for (int n = 0; n < NCH; ++n) {
-                qk_zero(xl[k][n]); qk_zero(xh[k][n]); qk_zero(yl[k][n]); qk_zero(yh[k][n]);
-                if (live && c[n].there) { qk_load(x + c[n].a0, xl[k][n]); qk_load(d + c[n].a0, yl[k][n]); }
-                if (live && c[n].second) { qk_load(x + c[n].a1, xh[k][n]); qk_load(d + c[n].a1, yh[k][n]); }
-            }
+        for (int n = 0; n < NCH; ++n) {
+            xa[n] = qk_f32<T, V>(xl[n]); xb[n] = qk_f32<T, V>(xr[n]);
+            ga[n] = qk_f32<T, V>(yl[n]); gb[n] = qk_f32<T, V>(yr[n]);
         }
+        const long now = at;
+        at = ahead;
+        ahead = position(t + 2 * step);
+        load(at);
+        f32x2 ss = make_f32x2(0.f, 0.f), dots = make_f32x2(0.f, 0.f);
 #pragma unroll
-        for (int k = 0; k < U; ++k) {
-            QkVec<V> xa[NCH], xb[NCH], ga[NCH], gb[NCH];
-            f32x2 ss = make_f32x2(0.f, 0.f), dots = make_f32x2(0.f, 0.f);
-#pragma unroll
-            for (int n = 0; n < NCH; ++n) {
-                xa[n] = qk_f32<T, V>(xl[k][n]); xb[n] = qk_f32<T, V>(xh[k][n]);
-                ga[n] = qk_f32<T, V>(yl[k][n]); gb[n] = qk_f32<T, V>(yh[k][n]);
-                if (pos[k] >= 0 && c[n].turned) {
-                    const float* angles = p.table + pos[k] * p.rot + c[n].rot0;
-                    qk_turn<V>(ga[n], gb[n], qk_params<V>(angles), qk_mul<V>(qk_params<V>(angles + p.rot / 2), qk_fill<V>(-1.f)), p.interleaved);
-                }
-                qk_dot<V>(ss, xa[n], xa[n]);
-                qk_dot<V>(ss, xb[n], xb[n]);
-                qk_dot<V>(dots, qk_mul<V>(ga[n], gain0[n]), xa[n]);
-                qk_dot<V>(dots, qk_mul<V>(gb[n], gain1[n]), xb[n]);
+        for (int n = 0; n < NCH; ++n) {
+            if (now >= 0 && c[n].turned) {
+                const float* angles = p.table + now * p.rot + c[n].rot0;
+                qk_turn<V>(ga[n], gb[n], qk_params<V>(angles), qk_mul<V>(qk_params<V>(angles + p.rot / 2), qk_fill<V>(-1.f)), p.interleaved);
             }
-            const float sum = qk_group_sum<G>(sum_f32x2(ss)), dot = qk_group_sum<G>(sum_f32x2(dots));
-            if (!out[k]) continue;
-            const float r = pos[k] >= 0 ? rsqrtf(fmaf(sum, inv_d, p.eps)) : 0.f;
-            const QkVec<V> rr = qk_fill<V>(r), m = qk_fill<V>(-(dot * inv_d * r * r * r));   // m: what dx has of x
-#pragma unroll
-            for (int n = 0; n < NCH; ++n) {
-                ga[n] = qk_mul<V>(ga[n], rr);
-                gb[n] = qk_mul<V>(gb[n], rr);
-                acc0[n] = qk_fma<V>(ga[n], xa[n], acc0[n]);
-                acc1[n] = qk_fma<V>(gb[n], xb[n], acc1[n]);
-                if (c[n].there) qk_store<T, V>(out[k] + c[n].a0, qk_fma<V>(m, xa[n], qk_mul<V>(ga[n], gain0[n])));
-                if (c[n].second) qk_store<T, V>(out[k] + c[n].a1, qk_fma<V>(m, xb[n], qk_mul<V>(gb[n], gain1[n])));
-            }
+            qk_dot<V>(ss, xa[n], xa[n]);
+            qk_dot<V>(ss, xb[n], xb[n]);
+            qk_dot<V>(dots, qk_mul<V>(ga[n], gain0[n]), xa[n]);
+            qk_dot<V>(dots, qk_mul<V>(gb[n], gain1[n]), xb[n]);
         }
+        const float sum = qk_group_sum<G>(sum_f32x2(ss)), dot = qk_group_sum<G>(sum_f32x2(dots));
+        const float r = now >= 0 ? rsqrtf(fmaf(sum, inv_d, p.eps)) : 0.f;
+        const QkVec<V> rr = qk_fill<V>(r), m = qk_fill<V>(-(dot * inv_d * r * r * r));   // m: what dx has of x
+#pragma unroll
+        for (int n = 0; n < NCH; ++n) {
+            ga[n] = qk_mul<V>(ga[n], rr);
+            gb[n] = qk_mul<V>(gb[n], rr);
+            acc0[n] = qk_fma<V>(ga[n], xa[n], acc0[n]);
+            acc1[n] = qk_fma<V>(gb[n], xb[n], acc1[n]);
+            if (head && c[n].there) qk_store<T, V>(out + c[n].a0, qk_fma<V>(m, xa[n], qk_mul<V>(ga[n], gain0[n])));
+            if (head && c[n].second) qk_store<T, V>(out + c[n].a1, qk_fma<V>(m, xb[n], qk_mul<V>(gb[n], gain1[n])));
+        }
+        out += o_inc;
     }
     // groups of the warp, then warps, in a fixed order
 #pragma unroll
@@ -376,12 +365,11 @@ qknorm_backward_kernel(const __grid_constant__ QkParams p) {
         }
     }
     __syncthreads();
-    float* const part = y.part + ((size_t)b * y.chunks + chunk) * p.D;
-    for (int d = threadIdx.x; d < p.D; d += QK_THREADS) {
+    float* const part = y.part + ((size_t)b * y.blocks * y.chunks + unit) * p.D;
+    for (int i = threadIdx.x; i < p.D; i += blockDim.x) {
         float s = 0.f;
-#pragma unroll
-        for (int w = 0; w < WARPS; ++w) s += qk_smem[w * p.D + d];
-        part[d] = s;
+        for (int w = 0; w < warps; ++w) s += qk_smem[w * p.D + i];
+        part[i] = s;
     }
 }
 
