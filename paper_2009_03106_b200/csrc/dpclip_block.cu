@@ -7,6 +7,7 @@
 
 #include "internal.cuh"
 #include "kernels_gated.cuh"
+#include "kernels_gated_f32.cuh"
 #include "kernels_qknorm.cuh"
 #include "kernels_relbias.cuh"
 #include "kernels_stored.cuh"
@@ -264,17 +265,18 @@ constexpr int kPairs = kNumSMs / 2;
 // pipeline and the last tile's epilogue; a 128-column tile's stage costs 0.6 of it (A is loaded for half the columns); splitting costs a launch
 // and the partial products' way to memory and back.
 struct GatedCut { int hn, splits, kb_per_split; };
-GatedCut gated_cut(long M, long cols, long KD, bool fwd) {
+// fp32: a stage is six products.
+GatedCut gated_cut(long M, long cols, long KD, bool fwd, bool f32) {
     const int KB = ceil_div(KD, tc::gt::BK);
     GatedCut best = {128, 1, KB};
     double least = 1e30;
     for (int hn = 64; hn <= 128; hn *= 2)
         for (int s = 1; s <= 32; s *= 2) {
-            if (s > 1 && KB < 4 * s) break;
+            if (s > 1 && KB < (f32 ? 2 : 4) * s) break;
             const long tiles = (long)ceil_div(M, 256) * ceil_div(cols, fwd ? hn : 2 * hn);
             if (s > 1 && tiles * s > 2 * kPairs) break;
             const int per = ceil_div(KB, s);
-            double cost = (double)((tiles * s + kPairs - 1) / kPairs) * (per * (hn == 128 ? 1.0 : 0.6) + 6);
+            double cost = (double)((tiles * s + kPairs - 1) / kPairs) * (per * (hn == 128 ? 1.0 : 0.6) * (f32 ? 6 : 1) + (f32 ? 12 : 6));
             if (s > 1) cost += 10 + (double)M * cols * (fwd ? 2 : 1) * 4 * (s + 1) / 5e6 / 0.28;
             if (cost < least) { least = cost; best = {hn, ceil_div(KB, per), per}; }
         }
@@ -287,17 +289,20 @@ inline int gated_simt_splits(long M, long cols, long KD, bool fwd) {
     return clamp_int(2L * kNumSMs / tiles, 1, clamp_int(KD / 128, 1, 32));
 }
 inline bool gated_rows_ok(const void* p, long ld) { return is_aligned(p, 16) && ld % 8 == 0; }
+// copies pay from here on: 2 x 2F x K x 2 bytes of copied weights against 4 M F K flops at the fp32 ALUs' rate
+constexpr int kGatedCopyRows = 32;
 inline long up8(long n) { return (n + 7) / 8 * 8; }
-struct GatedSpace { size_t part, copy_a, copy_w; };       // bytes: partial products; copies of an operand of M rows and of W
+// fp32 on the tensor cores: from here on the ALUs' 4 M K F at 32 TFLOP/s take longer than three launches and the planes' way to memory
+inline bool gated_planes(long M, long K, long F) { return M > kGatedCopyRows && (double)M * K * F > 1.5e8; }
+struct GatedSpace { size_t part, copy_a, copy_w; };       // bytes: partial products; copies (fp32: planes) of an operand of M rows and of W
 GatedSpace gated_space(long M, long K, long F, dpclip_dtype dtype, bool fwd) {
     const long cols = fwd ? F : K, KD = fwd ? K : 2 * F, width = fwd ? 2 * F : K;
-    const int simt = gated_simt_splits(M, cols, KD, fwd), tensor = dtype == DPCLIP_BF16 ? gated_cut(M, cols, KD, fwd).splits : 1;
+    const int simt = gated_simt_splits(M, cols, KD, fwd), tensor = gated_cut(M, cols, KD, fwd, dtype == DPCLIP_F32).splits;
     const int s = simt > tensor ? simt : tensor;
     GatedSpace g = {s > 1 ? round_up(sizeof(float) * (size_t)s * M * width, 256) : 0, 0, 0};
-    if (dtype == DPCLIP_BF16 && (K % 8 || F % 8)) {
-        g.copy_a = round_up(2 * (size_t)M * up8(KD), 256);
-        g.copy_w = round_up(2 * (size_t)2 * F * up8(K), 256);
-    }
+    const size_t planes = dtype == DPCLIP_F32 ? (gated_planes(M, K, F) ? 3 : 0) : K % 8 || F % 8 ? 1 : 0;
+    g.copy_a = planes * round_up(2 * (size_t)M * up8(KD), 256);
+    g.copy_w = planes * round_up(2 * (size_t)2 * F * up8(K), 256);
     return g;
 }
 inline size_t total_bytes(const GatedSpace& g) { return g.part + g.copy_a + g.copy_w; }
@@ -354,7 +359,7 @@ int launch_gated_tc(const tc::gt::Maps& maps, const tc::gt::Params& p, cudaStrea
 int gated_tensor(bool fwd, const void* a, long lda, const void* w, long ldw, int M, int K, int F, GatedOut out, int* status, cudaStream_t st) {
     using namespace tc::gt;
     const int KD = fwd ? K : 2 * F, cols = fwd ? F : K;
-    const GatedCut cut = gated_cut(M, cols, KD, fwd);
+    const GatedCut cut = gated_cut(M, cols, KD, fwd, false);
     Params p;
     memset(&p, 0, sizeof(p));
     p.KB = ceil_div(KD, BK);
@@ -385,8 +390,59 @@ int gated_tensor(bool fwd, const void* a, long lda, const void* w, long ldw, int
     if (keep) return cut.hn == 128 ? launch_gated_tc<true, true, 128>(maps, p, st) : launch_gated_tc<true, true, 64>(maps, p, st);
     return cut.hn == 128 ? launch_gated_tc<true, false, 128>(maps, p, st) : launch_gated_tc<true, false, 64>(maps, p, st);
 }
-// copies pay from here on: 2 x 2F x K x 2 bytes of copied weights against 4 M F K flops at the fp32 ALUs' rate
-constexpr int kGatedCopyRows = 32;
+
+int gated_split(const float* src, long ld, void* dst, long ldd, size_t plane_bytes, long rows, long cols, cudaStream_t st) {
+    const GatedSplit s = {src, ld, static_cast<__nv_bfloat16*>(dst), ldd, (long)(plane_bytes / 2), rows, (int)cols};
+    const int grid = clamp_int((rows * ((cols + 3) / 4) + 255) / 256, 1, kNumSMs * 16);
+    if (is_aligned(src, 16) && ld % 4 == 0 && cols % 4 == 0) gated_split_kernel<true><<<grid, 256, 0, st>>>(s);
+    else gated_split_kernel<false><<<grid, 256, 0, st>>>(s);
+    return finish_launch();
+}
+template <bool FWD, int HN>
+int launch_gated_tc3(const tc::gt3::Maps& maps, const tc::gt3::Params& p, cudaStream_t st) {
+    using C = tc::gt3::Cfg<HN>;
+    if (cudaFuncSetAttribute(tc::gated_tc3_kernel<FWD, HN>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM_BYTES) != cudaSuccess)
+        return DPCLIP_ERR_CUDA;
+    const int pairs = p.total < kPairs ? p.total : kPairs;
+    const int rc = launch_after(tc::gated_tc3_kernel<FWD, HN>, dim3(2 * pairs), tc::gt3::THREADS, C::SMEM_BYTES, st, maps, p);
+    return rc || p.out.splits == 1 ? rc : launch_gated_reduce<float, FWD>(p.out, st);
+}
+// a [M][KD], w [2F][K] in fp32; ws: the planes' place
+int gated_tensor_f32(bool fwd, const float* a, long lda, const float* w, long ldw, int M, int K, int F, GatedOut out, uint8_t* ws,
+                     const GatedSpace& space, int* status, cudaStream_t st) {
+    using namespace tc::gt3;
+    const int KD = fwd ? K : 2 * F, cols = fwd ? F : K;
+    const GatedCut cut = gated_cut(M, cols, KD, fwd, true);
+    uint8_t* const pa = ws + space.part, *const pw = pa + space.copy_a;
+    const size_t plane_a = space.copy_a / 3, plane_w = space.copy_w / 3;
+    int rc = gated_split(a, lda, pa, up8(KD), plane_a, M, KD, st);
+    if (!rc) rc = gated_split(w, ldw, pw, up8(K), plane_w, 2L * F, K, st);
+    if (rc) return rc;
+    Params p;
+    memset(&p, 0, sizeof(p));
+    p.KB = ceil_div(KD, BK);
+    p.kb_per_split = cut.kb_per_split;
+    p.tiles_m = ceil_div(M, 256); p.tiles_n = ceil_div(cols, fwd ? cut.hn : 2 * cut.hn);
+    const long total = (long)p.tiles_m * p.tiles_n * cut.splits;
+    if (total > 0x3FFFFFFFL) return DPCLIP_ERR_UNSUPPORTED;
+    p.total = (int)total;
+    p.status = status; p.out = out; p.out.splits = cut.splits;
+    p.vec_h = is_aligned(out.h, 16) && out.ldh % 4 == 0;
+    p.vec_z = out.z && is_aligned(out.z, 16) && out.ldz % 4 == 0 && F % 4 == 0;
+    Maps maps;
+    memset(&maps, 0, sizeof(maps));
+    bool ok = true;
+    for (int j = 0; j < 3; ++j) {
+        const __nv_bfloat16* wj = reinterpret_cast<const __nv_bfloat16*>(pw + j * plane_w);
+        ok = ok && encode_map_bf16(&maps.a[j], pa + j * plane_a, M, KD, up8(KD), 64, BM_CTA);
+        for (int r = 0; r < 2; ++r)
+            ok = ok && (fwd ? encode_map_bf16(&maps.b[r][j], wj + (long)r * F * up8(K), F, K, up8(K), 64, cut.hn)
+                            : encode_map_bf16(&maps.b[r][j], wj, 2L * F, K, up8(K), 64, BK));
+    }
+    if (!ok) return DPCLIP_ERR_CUDA;
+    if (fwd) return cut.hn == 128 ? launch_gated_tc3<true, 128>(maps, p, st) : launch_gated_tc3<true, 64>(maps, p, st);
+    return cut.hn == 128 ? launch_gated_tc3<false, 128>(maps, p, st) : launch_gated_tc3<false, 64>(maps, p, st);
+}
 
 int gated_check(int M, int K, int F, dpclip_dtype dtype, int act, bool product, const void* workspace, size_t workspace_bytes) {
     if (M <= 0 || K <= 0 || F <= 0 || F > (1 << 29) || !dtype_known(dtype) || act < DPCLIP_ACT_SILU || act > DPCLIP_ACT_RELU) return DPCLIP_ERR_INVALID_ARG;
@@ -585,6 +641,9 @@ int dpclip_gated_forward(const void* X, long ldx, const void* W, long ldw, const
             return gated_tensor(true, a, lda, w, ldb, M, K, F, out, static_cast<int*>(workspace), st);
         }
     }
+    if (dtype == DPCLIP_F32 && space.copy_w && tensor_cores_allowed())
+        return gated_tensor_f32(true, static_cast<const float*>(X), ldx, static_cast<const float*>(W), ldw, M, K, F, out, ws, space,
+                                static_cast<int*>(workspace), st);
     GatedSimt p;
     memset(&p, 0, sizeof(p));
     p.a = X; p.lda = ldx; p.w = W; p.ldw = ldw; p.M = M; p.N = F; p.KD = K; p.out = out;
@@ -631,6 +690,9 @@ int dpclip_gated_backward(const void* dH, long lddh, const void* Z, long ldz, co
         if (!w_ok) { w = ws + space.part + space.copy_a; ldb = up8(K); rc = gated_copy(W, ldw, ws + space.part + space.copy_a, ldb, 2L * F, K, st); if (rc) return rc; }
         return gated_tensor(false, a, dz_ok ? lddz : s.ldc, w, ldb, M, K, F, out, static_cast<int*>(workspace), st);
     }
+    if (dtype == DPCLIP_F32 && space.copy_w && tensor_cores_allowed())
+        return gated_tensor_f32(false, static_cast<const float*>(dZ), lddz, static_cast<const float*>(W), ldw, M, K, F, out, ws, space,
+                                static_cast<int*>(workspace), st);
     GatedSimt p;
     memset(&p, 0, sizeof(p));
     p.a = dZ; p.lda = lddz; p.w = W; p.ldw = ldw; p.M = M; p.N = K; p.KD = 2 * F; p.out = out;

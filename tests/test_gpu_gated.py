@@ -234,3 +234,49 @@ def test_block_in_one_step(dp, dtype, shape):
     torch.cuda.synchronize()
     check(C)
     assert dp.dpclip_read_status(ws) == 0
+
+
+@pytest.mark.parametrize("shape", [(600, 520, 500), (257, 1301, 460), (2000, 70, 1100), (130, 4100, 300), (90, 200, 8500), (5000, 64, 480)])
+@pytest.mark.parametrize("layout,with_bias", [("dense", True), ("odd", False), ("aligned", False)])
+def test_fp32_products_in_planes(dp, shape, layout, with_bias):
+    """Large fp32 calls: products of three bf16 planes each.  A window of 64 columns has 24 additions, each cut off (two units of 2^-24 of
+    what the window adds up); the windows are added up with rounding; the products left out are two more units."""
+    M, K, F = shape
+    g = torch.Generator().manual_seed(M + K)
+    X, W = torch.randn((M, K), generator=g), torch.randn((2 * F, K), generator=g) / math.sqrt(K)
+    bias = torch.randn((2 * F,), generator=g) if with_bias else None
+    x, w = X.double(), W.double()
+    z = x @ w.t() + (bias.double() if with_bias else 0)
+    mag = x.abs() @ w.abs().t() + (bias.double().abs() if with_bias else 0)
+    ws = workspace(dp, dp.dpclip_gated_workspace_bytes(M, K, F, 0))
+    pad = {"dense": 0, "odd": 1, "aligned": 4}[layout]
+    H, check_h = guarded((M, F), F32, strides=(F + pad, 1))
+    Z, check_z = guarded((M, 2 * F), F32, strides=(2 * F + pad, 1))
+    dev = rows(X, layout, F32), rows(W, layout, F32)
+    before = dp.dpclip_launch_count()
+    dp.dpclip_gated_forward(*dev, None if bias is None else bias.cuda(), H, Z, dp.DPCLIP_ACT_GELU, ws)
+    assert dp.dpclip_launch_count() - before >= 3                  # two splits and the product: not the fp32-ALU form
+    torch.cuda.synchronize()
+    assert dp.dpclip_read_status(ws) == 0
+    check_h(); check_z()
+    tol = (48 + math.ceil(K / 64) + 8) * U32 * mag
+    close(Z, z, tol + U32 * z.abs())
+    a, _ = act_and_slope(z[:, :F], "gelu")
+    zu, dg, du = z[:, F:], tol[:, :F], tol[:, F:]
+    close(H, a * zu, U32 * 1.01 * (a * zu).abs() + 1.2 * (zu.abs() + du) * dg + a.abs() * du + fast(F32, z[:, :F]) * (z[:, :F] * zu).abs() + 1e-37)
+    dH = torch.randn((M, F), generator=g)
+    dZ, check_z = guarded((M, 2 * F), F32, strides=(2 * F + pad, 1))
+    dX, check_x = guarded((M, K), F32, strides=(K + pad, 1))
+    dp.dpclip_gated_backward(rows(dH, layout, F32), Z, dev[1], dZ, dX, dp.DPCLIP_ACT_GELU, ws)
+    torch.cuda.synchronize()
+    assert dp.dpclip_read_status(ws) == 0
+    check_z(); check_x()
+    got = dZ.double().cpu()
+    dx = got @ w
+    # a split contraction adds up to 32 partial products more
+    close(dX, dx, (48 + math.ceil(2 * F / 64) + 40) * U32 * (got.abs() @ w.abs()) + U32 * dx.abs())
+    # an infinity or a NaN of an input does not get lost
+    X[3, 5] = float("inf"); X[7, 2] = float("nan")
+    dp.dpclip_gated_forward(rows(X, layout, F32), dev[1], None, H, Z, dp.DPCLIP_ACT_GELU, ws)
+    bad = ~torch.isfinite(Z)
+    assert bool(bad[3].all()) and bool(bad[7].all()) and not bool(bad[8].any()) and not bool(bad[2].any())
