@@ -293,7 +293,7 @@ inline bool gated_rows_ok(const void* p, long ld) { return is_aligned(p, 16) && 
 constexpr int kGatedCopyRows = 32;
 inline long up8(long n) { return (n + 7) / 8 * 8; }
 // fp32 on the tensor cores: from here on the ALUs' 4 M K F at 32 TFLOP/s take longer than three launches and the planes' way to memory
-inline bool gated_planes(long M, long K, long F) { return M > kGatedCopyRows && (double)M * K * F > 1.5e8; }
+inline bool gated_planes(long M, long K, long F) { return M > kGatedCopyRows && (double)M * K * F > 6e7; }
 struct GatedSpace { size_t part, copy_a, copy_w; };       // bytes: partial products; copies (fp32: planes) of an operand of M rows and of W
 GatedSpace gated_space(long M, long K, long F, dpclip_dtype dtype, bool fwd) {
     const long cols = fwd ? F : K, KD = fwd ? K : 2 * F, width = fwd ? 2 * F : K;
@@ -307,8 +307,14 @@ GatedSpace gated_space(long M, long K, long F, dpclip_dtype dtype, bool fwd) {
 }
 inline size_t total_bytes(const GatedSpace& g) { return g.part + g.copy_a + g.copy_w; }
 
-int gated_copy(const void* src, long ld, void* dst, long ldd, long rows, long cols, cudaStream_t st) {
-    gated_copy_kernel<<<clamp_int(rows, 1, kNumSMs * 16), 256, 0, st>>>(static_cast<const __nv_bfloat16*>(src), ld, static_cast<__nv_bfloat16*>(dst), ldd, rows, (int)cols);
+// copies of up to two matrices in one launch; none: nothing
+int gated_copies(const GatedCopy* c, int n_copies, cudaStream_t st) {
+    if (n_copies == 0) return DPCLIP_OK;
+    GatedCopies p;
+    memset(&p, 0, sizeof(p));
+    long n = 0;
+    for (int k = 0; k < n_copies; ++k) { p.c[k] = c[k]; n += c[k].rows * ((c[k].cols + 7) / 8); if (k == 0) p.first = n; }
+    gated_copy_kernel<<<clamp_int((n + 255) / 256, 1, kNumSMs * 16), 256, 0, st>>>(p, n);
     return finish_launch();
 }
 
@@ -351,8 +357,7 @@ int launch_gated_tc(const tc::gt::Maps& maps, const tc::gt::Params& p, cudaStrea
     if (cudaFuncSetAttribute(tc::gated_tc_kernel<FWD, KEEP, HN>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM_BYTES) != cudaSuccess)
         return DPCLIP_ERR_CUDA;
     const int pairs = p.total < kPairs ? p.total : kPairs;
-    tc::gated_tc_kernel<FWD, KEEP, HN><<<2 * pairs, C::THREADS, C::SMEM_BYTES, st>>>(maps, p);
-    const int rc = finish_launch();
+    const int rc = launch_after(tc::gated_tc_kernel<FWD, KEEP, HN>, dim3(2 * pairs), C::THREADS, C::SMEM_BYTES, st, maps, p);
     return rc || p.out.splits == 1 ? rc : launch_gated_reduce<__nv_bfloat16, FWD>(p.out, st);
 }
 // a [M][KD] (lda), w [2F][K] (ldw): rows TMA can address
@@ -391,11 +396,17 @@ int gated_tensor(bool fwd, const void* a, long lda, const void* w, long ldw, int
     return cut.hn == 128 ? launch_gated_tc<true, false, 128>(maps, p, st) : launch_gated_tc<true, false, 64>(maps, p, st);
 }
 
-int gated_split(const float* src, long ld, void* dst, long ldd, size_t plane_bytes, long rows, long cols, cudaStream_t st) {
-    const GatedSplit s = {src, ld, static_cast<__nv_bfloat16*>(dst), ldd, (long)(plane_bytes / 2), rows, (int)cols};
-    const int grid = clamp_int((rows * ((cols + 3) / 4) + 255) / 256, 1, kNumSMs * 16);
-    if (is_aligned(src, 16) && ld % 4 == 0 && cols % 4 == 0) gated_split_kernel<true><<<grid, 256, 0, st>>>(s);
-    else gated_split_kernel<false><<<grid, 256, 0, st>>>(s);
+int gated_splits(const GatedSplit* c, int n_splits, cudaStream_t st) {
+    GatedSplits p;
+    memset(&p, 0, sizeof(p));
+    long n = 0;
+    for (int k = 0; k < n_splits; ++k) {
+        p.c[k] = c[k];
+        p.c[k].vec = is_aligned(c[k].src, 16) && c[k].ld % 4 == 0 && c[k].cols % 4 == 0;
+        n += c[k].rows * ((c[k].cols + 3) / 4);
+        if (k == 0) p.first = n;
+    }
+    gated_split_kernel<<<clamp_int((n + 255) / 256, 1, kNumSMs * 16), 256, 0, st>>>(p, n);
     return finish_launch();
 }
 template <bool FWD, int HN>
@@ -407,17 +418,13 @@ int launch_gated_tc3(const tc::gt3::Maps& maps, const tc::gt3::Params& p, cudaSt
     const int rc = launch_after(tc::gated_tc3_kernel<FWD, HN>, dim3(2 * pairs), tc::gt3::THREADS, C::SMEM_BYTES, st, maps, p);
     return rc || p.out.splits == 1 ? rc : launch_gated_reduce<float, FWD>(p.out, st);
 }
-// a [M][KD], w [2F][K] in fp32; ws: the planes' place
-int gated_tensor_f32(bool fwd, const float* a, long lda, const float* w, long ldw, int M, int K, int F, GatedOut out, uint8_t* ws,
-                     const GatedSpace& space, int* status, cudaStream_t st) {
+// The product of planes that lie in the workspace behind the partial products: those of a [M][KD], then those of w [2F][K].
+int gated_tensor_f32(bool fwd, int M, int K, int F, GatedOut out, uint8_t* ws, const GatedSpace& space, int* status, cudaStream_t st) {
     using namespace tc::gt3;
     const int KD = fwd ? K : 2 * F, cols = fwd ? F : K;
     const GatedCut cut = gated_cut(M, cols, KD, fwd, true);
     uint8_t* const pa = ws + space.part, *const pw = pa + space.copy_a;
     const size_t plane_a = space.copy_a / 3, plane_w = space.copy_w / 3;
-    int rc = gated_split(a, lda, pa, up8(KD), plane_a, M, KD, st);
-    if (!rc) rc = gated_split(w, ldw, pw, up8(K), plane_w, 2L * F, K, st);
-    if (rc) return rc;
     Params p;
     memset(&p, 0, sizeof(p));
     p.KB = ceil_div(KD, BK);
@@ -636,14 +643,22 @@ int dpclip_gated_forward(const void* X, long ldx, const void* W, long ldw, const
         if (as_is || (space.copy_w && M > kGatedCopyRows)) {
             const void* a = X; const void* w = W;
             long lda = ldx, ldb = ldw;
-            if (!gated_rows_ok(X, ldx)) { a = ws + space.part; lda = up8(K); rc = gated_copy(X, ldx, ws + space.part, lda, M, K, st); if (rc) return rc; }
-            if (!gated_rows_ok(W, ldw)) { w = ws + space.part + space.copy_a; ldb = up8(K); rc = gated_copy(W, ldw, ws + space.part + space.copy_a, ldb, 2L * F, K, st); if (rc) return rc; }
+            GatedCopy c[2];
+            int n = 0;
+            if (!gated_rows_ok(X, ldx)) { a = ws + space.part; lda = up8(K); c[n++] = {static_cast<const __nv_bfloat16*>(X), ldx, (__nv_bfloat16*)a, lda, M, K}; }
+            if (!gated_rows_ok(W, ldw)) { w = ws + space.part + space.copy_a; ldb = up8(K); c[n++] = {static_cast<const __nv_bfloat16*>(W), ldw, (__nv_bfloat16*)w, ldb, 2L * F, K}; }
+            rc = gated_copies(c, n, st);
+            if (rc) return rc;
             return gated_tensor(true, a, lda, w, ldb, M, K, F, out, static_cast<int*>(workspace), st);
         }
     }
-    if (dtype == DPCLIP_F32 && space.copy_w && tensor_cores_allowed())
-        return gated_tensor_f32(true, static_cast<const float*>(X), ldx, static_cast<const float*>(W), ldw, M, K, F, out, ws, space,
-                                static_cast<int*>(workspace), st);
+    if (dtype == DPCLIP_F32 && space.copy_w && tensor_cores_allowed()) {
+        uint8_t* const pa = ws + space.part, *const pw = pa + space.copy_a;
+        const GatedSplit c[2] = {{static_cast<const float*>(X), ldx, (__nv_bfloat16*)pa, up8(K), (long)(space.copy_a / 6), M, K, 0},
+                                 {static_cast<const float*>(W), ldw, (__nv_bfloat16*)pw, up8(K), (long)(space.copy_w / 6), 2L * F, K, 0}};
+        rc = gated_splits(c, 2, st);
+        return rc ? rc : gated_tensor_f32(true, M, K, F, out, ws, space, static_cast<int*>(workspace), st);
+    }
     GatedSimt p;
     memset(&p, 0, sizeof(p));
     p.a = X; p.lda = ldx; p.w = W; p.ldw = ldw; p.M = M; p.N = F; p.KD = K; p.out = out;
@@ -662,14 +677,27 @@ int dpclip_gated_backward(const void* dH, long lddh, const void* Z, long ldz, co
     const GatedSpace space = gated_space(M, K, F, dtype, false);
     uint8_t* const ws = static_cast<uint8_t*>(workspace) + kHeaderBytes;
     const bool dz_ok = gated_rows_ok(dZ, lddz), w_ok = dX && gated_rows_ok(W, ldw);
+    const bool planes = dX && dtype == DPCLIP_F32 && space.copy_w && tensor_cores_allowed();
     const bool tensor = dX && dtype == DPCLIP_BF16 && tensor_cores_allowed() && ((dz_ok && w_ok) || (space.copy_w && M > kGatedCopyRows));
+    uint8_t* const pa = ws + space.part, *const pw = pa + space.copy_a;
+    // W first: the product then follows the kernel that writes dZ
+    if (planes) {
+        const GatedSplit c = {static_cast<const float*>(W), ldw, (__nv_bfloat16*)pw, up8(K), (long)(space.copy_w / 6), 2L * F, K, 0};
+        rc = gated_splits(&c, 1, st);
+    } else if (tensor && !w_ok) {
+        const GatedCopy c = {static_cast<const __nv_bfloat16*>(W), ldw, (__nv_bfloat16*)pw, up8(K), 2L * F, K};
+        rc = gated_copies(&c, 1, st);
+    }
+    if (rc) return rc;
     GatedSignal s;
     memset(&s, 0, sizeof(s));
     s.dh = dH; s.lddh = lddh; s.z = Z; s.ldz = ldz; s.dz = dZ; s.lddz = lddz; s.M = M; s.F = F; s.act = act;
-    if (tensor && !dz_ok) { s.copy = ws + space.part; s.ldc = up8(2L * F); }
+    if (planes || (tensor && !dz_ok)) { s.copy = (__nv_bfloat16*)pa; s.ldc = up8(2L * F); s.plane = (long)(space.copy_a / 6); }
     const long v = dtype == DPCLIP_F32 ? 4 : 8;
     const bool vec = is_aligned(dH, 16) && is_aligned(Z, 16) && is_aligned(dZ, 16) && F % v == 0 && lddh % v == 0 && ldz % v == 0 && lddz % v == 0;
-    const int grid = clamp_int(M, 1, kNumSMs * 8);
+    s.per_row = vec ? F / (int)v : F;
+    const int tall = s.per_row < 256 ? 256 / s.per_row : 1;
+    const int grid = clamp_int(((long)M + tall - 1) / tall, 1, kNumSMs * 8);
     if (dtype == DPCLIP_F32) {
         if (vec) gated_signal_kernel<float, 4><<<grid, 256, 0, st>>>(s);
         else gated_signal_kernel<float, 1><<<grid, 256, 0, st>>>(s);
@@ -684,15 +712,10 @@ int dpclip_gated_backward(const void* dH, long lddh, const void* Z, long ldz, co
     out.h = dX; out.ldh = lddx; out.M = M; out.F = K; out.splits = 1;
     out.part = reinterpret_cast<float*>(ws);
     if (tensor) {
-        const void* a = dz_ok ? dZ : s.copy;
-        const void* w = W;
-        long ldb = ldw;
-        if (!w_ok) { w = ws + space.part + space.copy_a; ldb = up8(K); rc = gated_copy(W, ldw, ws + space.part + space.copy_a, ldb, 2L * F, K, st); if (rc) return rc; }
-        return gated_tensor(false, a, dz_ok ? lddz : s.ldc, w, ldb, M, K, F, out, static_cast<int*>(workspace), st);
+        return gated_tensor(false, dz_ok ? dZ : s.copy, dz_ok ? lddz : s.ldc, w_ok ? W : pw, w_ok ? ldw : up8(K), M, K, F, out,
+                            static_cast<int*>(workspace), st);
     }
-    if (dtype == DPCLIP_F32 && space.copy_w && tensor_cores_allowed())
-        return gated_tensor_f32(false, static_cast<const float*>(dZ), lddz, static_cast<const float*>(W), ldw, M, K, F, out, ws, space,
-                                static_cast<int*>(workspace), st);
+    if (planes) return gated_tensor_f32(false, M, K, F, out, ws, space, static_cast<int*>(workspace), st);
     GatedSimt p;
     memset(&p, 0, sizeof(p));
     p.a = dZ; p.lda = lddz; p.w = W; p.ldw = ldw; p.M = M; p.N = K; p.KD = 2 * F; p.out = out;

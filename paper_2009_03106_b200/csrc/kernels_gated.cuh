@@ -88,26 +88,49 @@ __device__ __forceinline__ void gate_store(float* p, float v) { *p = v; }
 __device__ __forceinline__ void gate_store(__nv_bfloat16* p, float v) { *p = __float2bfloat16_rn(v); }
 
 // ------------------------------------------------------------------------------------------------ dz from dh and z
+// fp32 as three bf16 planes (kernels_gated_f32.cuh): the top 8 significant bits, the next 8, the last 8, each cut off, so that they add up to
+// the number and nothing overflows.  An infinity or a NaN stays in the first plane.
+__device__ __forceinline__ void split3(float x, uint16_t (&t)[3]) {
+    const uint32_t h = __float_as_uint(x) & 0xFFFF0000u;
+    const float r = (h & 0x7F800000u) == 0x7F800000u ? 0.f : x - __uint_as_float(h);
+    const uint32_t m = __float_as_uint(r) & 0xFFFF0000u;
+    const float l = r - __uint_as_float(m);
+    t[0] = (uint16_t)(h >> 16) | (uint16_t)(x != x ? 0x40 : 0);    // a NaN whose payload lies in the low bits alone must not become an infinity
+    t[1] = (uint16_t)(m >> 16);
+    t[2] = (uint16_t)(__float_as_uint(l) >> 16);
+}
 struct GatedSignal {
     const void* dh; long lddh;
     const void* z; long ldz;             // [M][2F]
     void* dz; long lddz;                 // [M][2F], may be z
-    void* copy; long ldc;                // NULL, or a second place for dz with 16-byte rows
-    long M; int F, act;
+    __nv_bfloat16* copy; long ldc;       // NULL, or rows of 16-byte multiples for the product: bf16 a copy of dz, fp32 its three planes
+    long plane;
+    long M; int F, act, per_row;         // per_row: groups of V elements a row of h
 };
+template <typename T> __device__ __forceinline__ void gated_copy_out(const GatedSignal& p, long m, int f, float v) {
+    __nv_bfloat16* const to = p.copy + m * p.ldc + f;
+    if constexpr (sizeof(T) == 2) *to = __float2bfloat16_rn(v);
+    else {
+        uint16_t t[3];
+        split3(v, t);
+#pragma unroll
+        for (int j = 0; j < 3; ++j) *reinterpret_cast<uint16_t*>(to + j * p.plane) = t[j];
+    }
+}
+// 256 threads: as many rows side by side as fit, a row's groups along the threads.
 template <typename T, int V>             // V elements a thread: 16 bytes, or one
 __global__ void __launch_bounds__(256)
 gated_signal_kernel(const __grid_constant__ GatedSignal p) {
     constexpr bool EXACT = sizeof(T) == 4;
-    const int per_row = (p.F + V - 1) / V;
-    const uint32_t row_step = gridDim.x;
+    griddep_launch_dependents();
+    const int wide = min(p.per_row, 256), tall = 256 / wide, ty = threadIdx.x / wide, tx = threadIdx.x - ty * wide;
+    if (ty >= tall) return;
     gate_dispatch<EXACT>(p.act, [&](auto a) {
         constexpr int ACT = decltype(a)::value;
-        for (long m = blockIdx.x; m < p.M; m += row_step) {
+        for (long m = (long)blockIdx.x * tall + ty; m < p.M; m += (long)gridDim.x * tall) {
             const T* const dh = static_cast<const T*>(p.dh) + m * p.lddh;
             const T* const zg = static_cast<const T*>(p.z) + m * p.ldz;
             T* const og = static_cast<T*>(p.dz) + m * p.lddz;
-            T* const oc = p.copy ? static_cast<T*>(p.copy) + m * p.ldc : nullptr;
             auto one = [&](float h, float g, float u, float& dg, float& du) {
                 float act, slope;
                 gate_act_grad<ACT, EXACT>(g, act, slope);
@@ -116,15 +139,15 @@ gated_signal_kernel(const __grid_constant__ GatedSignal p) {
             };
             if constexpr (V == 1) {
 #pragma unroll 4
-                for (int f = threadIdx.x; f < per_row; f += 256) {
+                for (int f = tx; f < p.per_row; f += wide) {
                     float dg, du;
                     one(to_f32(dh[f]), to_f32(zg[f]), to_f32(zg[p.F + f]), dg, du);
                     gate_store(og + f, dg); gate_store(og + p.F + f, du);
-                    if (oc) { gate_store(oc + f, dg); gate_store(oc + p.F + f, du); }
+                    if (p.copy) { gated_copy_out<T>(p, m, f, dg); gated_copy_out<T>(p, m, p.F + f, du); }
                 }
             } else {
 #pragma unroll 2
-                for (int c = threadIdx.x; c < per_row; c += 256) {
+                for (int c = tx; c < p.per_row; c += wide) {
                     const int f = c * V;
                     const uint4 h = *reinterpret_cast<const uint4*>(dh + f), g = *reinterpret_cast<const uint4*>(zg + f),
                                 u = *reinterpret_cast<const uint4*>(zg + p.F + f);
@@ -132,8 +155,9 @@ gated_signal_kernel(const __grid_constant__ GatedSignal p) {
                     uint32_t a[4], b[4];
 #pragma unroll
                     for (int k = 0; k < 4; ++k) {
-                        float x0, x1, y0, y1;
+                        float x0, y0;
                         if constexpr (V == 8) {
+                            float x1, y1;
                             one(__uint_as_float(hw[k] << 16), __uint_as_float(gw[k] << 16), __uint_as_float(uw[k] << 16), x0, y0);
                             one(__uint_as_float(hw[k] & 0xFFFF0000u), __uint_as_float(gw[k] & 0xFFFF0000u), __uint_as_float(uw[k] & 0xFFFF0000u), x1, y1);
                             a[k] = f32x2_to_bf16x2(make_f32x2(x0, x1));
@@ -145,18 +169,42 @@ gated_signal_kernel(const __grid_constant__ GatedSignal p) {
                     }
                     *reinterpret_cast<uint4*>(og + f) = make_uint4(a[0], a[1], a[2], a[3]);
                     *reinterpret_cast<uint4*>(og + p.F + f) = make_uint4(b[0], b[1], b[2], b[3]);
+                    if constexpr (V == 4) {
+                        if (p.copy) {
+#pragma unroll
+                            for (int half = 0; half < 2; ++half) {
+                                uint16_t t[4][3];
+#pragma unroll
+                                for (int k = 0; k < 4; ++k) split3(__uint_as_float(half ? b[k] : a[k]), t[k]);
+#pragma unroll
+                                for (int j = 0; j < 3; ++j)
+                                    *reinterpret_cast<uint2*>(p.copy + j * p.plane + m * p.ldc + half * p.F + f) =
+                                        make_uint2(t[0][j] | (uint32_t)t[1][j] << 16, t[2][j] | (uint32_t)t[3][j] << 16);
+                            }
+                        }
+                    }
                 }
             }
         }
     });
 }
 
-// rows of any stride and start copied to rows of 16-byte multiples
+// Rows of any stride and start copied to rows of 16-byte multiples: eight elements a thread, stored at once.  Two matrices a launch.
+struct GatedCopy { const __nv_bfloat16* src; long ld; __nv_bfloat16* dst; long ldd, rows; int cols; };
+struct GatedCopies { GatedCopy c[2]; long first; };          // first: groups of the first matrix
 __global__ void __launch_bounds__(256)
-gated_copy_kernel(const __nv_bfloat16* __restrict__ src, long ld, __nv_bfloat16* __restrict__ dst, long ldd, long rows, int cols) {
-    for (long m = blockIdx.x; m < rows; m += gridDim.x) {
-#pragma unroll 4
-        for (int c = threadIdx.x; c < cols; c += 256) dst[m * ldd + c] = src[m * ld + c];
+gated_copy_kernel(const __grid_constant__ GatedCopies p, long n) {
+    griddep_launch_dependents();
+    for (long i = (long)blockIdx.x * 256 + threadIdx.x; i < n; i += (long)gridDim.x * 256) {
+        const GatedCopy& y = p.c[i >= p.first];
+        const uint32_t per = (uint32_t)(y.cols + 7) >> 3;
+        const long k = i >= p.first ? i - p.first : i, m = k / per;
+        const int c = (int)(k - m * per) * 8;
+        const __nv_bfloat16* s = y.src + m * y.ld + c;
+        uint16_t t[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) t[j] = c + j < y.cols ? *reinterpret_cast<const uint16_t*>(s + j) : (uint16_t)0;
+        *reinterpret_cast<uint4*>(y.dst + m * y.ldd + c) = make_uint4(t[0] | (uint32_t)t[1] << 16, t[2] | (uint32_t)t[3] << 16, t[4] | (uint32_t)t[5] << 16, t[6] | (uint32_t)t[7] << 16);
     }
 }
 
@@ -484,7 +532,8 @@ gated_tc_kernel(const __grid_constant__ gt::Maps maps, const __grid_constant__ g
     cluster_sync_all();
     tc_fence_after_sync();
     const uint32_t tmem_base = *tmem_slot;
-    griddep_wait();                      // operands that a launch in front of this one has laid out
+    griddep_wait();                      // operands that a launch in front of this one has written
+    griddep_launch_dependents();
 
     if (warp == 0) {
         if (lane == 0) {

@@ -16,42 +16,32 @@
 
 namespace dpclip {
 
-// src [rows][cols] fp32 -> planes dst + k * plane, rows of ldd (a multiple of 8)
-struct GatedSplit { const float* src; long ld; __nv_bfloat16* dst; long ldd, plane, rows; int cols; };
-__device__ __forceinline__ void split3(float x, uint16_t (&t)[3]) {
-    const uint32_t h = __float_as_uint(x) & 0xFFFF0000u;
-    // an infinity or a NaN stays in the first plane
-    const float r = (h & 0x7F800000u) == 0x7F800000u ? 0.f : x - __uint_as_float(h);
-    const uint32_t m = __float_as_uint(r) & 0xFFFF0000u;
-    const float l = r - __uint_as_float(m);
-    // a NaN whose payload lies in the low bits alone must not become an infinity
-    t[0] = (uint16_t)(h >> 16) | (uint16_t)(x != x ? 0x40 : 0);
-    t[1] = (uint16_t)(m >> 16);
-    t[2] = (uint16_t)(__float_as_uint(l) >> 16);
-}
-template <bool VEC>
+// src [rows][cols] fp32 -> planes dst + k * plane, rows of ldd (a multiple of 8).  Two matrices a launch.
+struct GatedSplit { const float* src; long ld; __nv_bfloat16* dst; long ldd, plane, rows; int cols, vec; };
+struct GatedSplits { GatedSplit c[2]; long first; };         // first: groups of four of the first matrix
 __global__ void __launch_bounds__(256)
-gated_split_kernel(const __grid_constant__ GatedSplit p) {
-    const int per = (p.cols + 3) >> 2;
-    const long n = p.rows * per;
+gated_split_kernel(const __grid_constant__ GatedSplits p, long n) {
+    griddep_launch_dependents();
     for (long i = (long)blockIdx.x * 256 + threadIdx.x; i < n; i += (long)gridDim.x * 256) {
-        const long m = i / per;
-        const int c = (int)(i - m * per) * 4;
-        const float* s = p.src + m * p.ld + c;
+        const GatedSplit& y = p.c[i >= p.first];
+        const uint32_t per = (uint32_t)(y.cols + 3) >> 2;
+        const long k = i >= p.first ? i - p.first : i, m = k / per;
+        const int c = (int)(k - m * per) * 4;
+        const float* s = y.src + m * y.ld + c;
         float x[4];
-        if (VEC) {
+        if (y.vec) {
             const float4 v = *reinterpret_cast<const float4*>(s);
             x[0] = v.x; x[1] = v.y; x[2] = v.z; x[3] = v.w;
         } else {
 #pragma unroll
-            for (int k = 0; k < 4; ++k) x[k] = c + k < p.cols ? s[k] : 0.f;
+            for (int j = 0; j < 4; ++j) x[j] = c + j < y.cols ? s[j] : 0.f;
         }
         uint16_t t[4][3];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) split3(x[k], t[k]);
+        for (int j = 0; j < 4; ++j) split3(x[j], t[j]);
 #pragma unroll
         for (int j = 0; j < 3; ++j)
-            *reinterpret_cast<uint2*>(p.dst + j * p.plane + m * p.ldd + c) =
+            *reinterpret_cast<uint2*>(y.dst + j * y.plane + m * y.ldd + c) =
                 make_uint2(t[0][j] | (uint32_t)t[1][j] << 16, t[2][j] | (uint32_t)t[3][j] << 16);
     }
 }
@@ -225,19 +215,21 @@ gated_tc3_kernel(const __grid_constant__ gt3::Maps maps, const __grid_constant__
 #pragma unroll
                 for (int j = 0; j < 4; ++j) mine[lane * 4 + (j ^ ((lane >> 1) & 3))] = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
                 __syncwarp();
+                if (vec && col + 16 <= o.F) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int r = i * 8 + (lane >> 2), s = lane & 3, c = col + s * 4;
-                    const float4 q = mine[r * 4 + (s ^ ((r >> 1) & 3))];
-                    if (row0 + r < o.M) {
-                        float* to = base + (long)(row0 + r) * ld + c;
-                        if (vec && c + 4 <= o.F) *reinterpret_cast<float4*>(to) = q;
-                        else {
-                            if (c < o.F) to[0] = q.x;
-                            if (c + 1 < o.F) to[1] = q.y;
-                            if (c + 2 < o.F) to[2] = q.z;
-                            if (c + 3 < o.F) to[3] = q.w;
-                        }
+                    for (int i = 0; i < 4; ++i) {
+                        const int r = i * 8 + (lane >> 2), s = lane & 3;
+                        if (row0 + r < o.M) *reinterpret_cast<float4*>(base + (long)(row0 + r) * ld + col + s * 4) = mine[r * 4 + (s ^ ((r >> 1) & 3))];
+                    }
+                } else {
+                    // rows at any address, or the last columns: one element a lane, sixteen lanes a row
+                    const float* const flat = reinterpret_cast<const float*>(mine);
+                    const int s = lane & 15, c = col + s;
+#pragma unroll 4
+                    for (int i = 0; i < 16; ++i) {
+                        const int r = i * 2 + (lane >> 4);
+                        const float q = flat[r * 16 + (((s >> 2) ^ ((r >> 1) & 3)) << 2) + (s & 3)];
+                        if (row0 + r < o.M && c < o.F) base[(long)(row0 + r) * ld + c] = q;
                     }
                 }
                 __syncwarp();
