@@ -294,19 +294,12 @@ constexpr int kGatedCopyRows = 32;
 inline long up8(long n) { return (n + 7) / 8 * 8; }
 // fp32 on the tensor cores: from here on the ALUs' 4 M K F at 32 TFLOP/s take longer than three launches and the planes' way to memory
 inline bool gated_planes(long M, long K, long F) { return M > kGatedCopyRows && (double)M * K * F > 6e7; }
-// dz inside the launch of its product: where the product runs in 256-column tiles, unsplit, for at least a few waves of them, and dz is too
-// large to wait for in L2 (32768 x 1024 x 4096: XX us, two launches YY)
-inline bool gated_fuse(long M, long K, long F) {
-    const GatedCut cut = gated_cut(M, K, 2 * F, false, false);
-    return cut.hn == 128 && cut.splits == 1 && (long)ceil_div(M, 256) * ceil_div(K, 256) >= 2 * kPairs && M * F >= (1L << 24);
-}
 struct GatedSpace { size_t part, copy_a, copy_w; };       // bytes: partial products; copies (fp32: planes) of an operand of M rows and of W
 GatedSpace gated_space(long M, long K, long F, dpclip_dtype dtype, bool fwd) {
     const long cols = fwd ? F : K, KD = fwd ? K : 2 * F, width = fwd ? 2 * F : K;
     const int simt = gated_simt_splits(M, cols, KD, fwd), tensor = gated_cut(M, cols, KD, fwd, dtype == DPCLIP_F32).splits;
     const int s = simt > tensor ? simt : tensor;
     GatedSpace g = {s > 1 ? round_up(sizeof(float) * (size_t)s * M * width, 256) : 0, 0, 0};
-    if (!fwd && dtype == DPCLIP_BF16 && gated_fuse(M, K, F) && g.part < 4 * (size_t)(M / 256 + 2)) g.part = round_up(4 * (size_t)(M / 256 + 2), 256);
     const size_t planes = dtype == DPCLIP_F32 ? (gated_planes(M, K, F) ? 3 : 0) : K % 8 || F % 8 ? 1 : 0;
     g.copy_a = planes * round_up(2 * (size_t)M * up8(KD), 256);
     g.copy_w = planes * round_up(2 * (size_t)2 * F * up8(K), 256);
@@ -358,23 +351,17 @@ int launch_gated_few(const GatedFew& p, cudaStream_t st) {
          : M <= 4 ? launch_gated_few<T, V, 4>(p, st) : launch_gated_few<T, V, 8>(p, st);
 }
 
-template <bool FWD, bool KEEP, int HN, bool FUSE = false>
+template <bool FWD, bool KEEP, int HN>
 int launch_gated_tc(const tc::gt::Maps& maps, const tc::gt::Params& p, cudaStream_t st) {
-    using C = tc::gt::Cfg<FWD, KEEP, HN, FUSE>;
-    if (cudaFuncSetAttribute(tc::gated_tc_kernel<FWD, KEEP, HN, FUSE>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM_BYTES) != cudaSuccess)
+    using C = tc::gt::Cfg<FWD, KEEP, HN>;
+    if (cudaFuncSetAttribute(tc::gated_tc_kernel<FWD, KEEP, HN>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM_BYTES) != cudaSuccess)
         return DPCLIP_ERR_CUDA;
     const int pairs = p.total < kPairs ? p.total : kPairs;
-    if (FUSE) {                                            // behind a clear of its counters, not behind a kernel
-        tc::gated_tc_kernel<FWD, KEEP, HN, FUSE><<<2 * pairs, C::THREADS, C::SMEM_BYTES, st>>>(maps, p);
-        return finish_launch();
-    }
-    const int rc = launch_after(tc::gated_tc_kernel<FWD, KEEP, HN, FUSE>, dim3(2 * pairs), C::THREADS, C::SMEM_BYTES, st, maps, p);
+    const int rc = launch_after(tc::gated_tc_kernel<FWD, KEEP, HN>, dim3(2 * pairs), C::THREADS, C::SMEM_BYTES, st, maps, p);
     return rc || p.out.splits == 1 ? rc : launch_gated_reduce<__nv_bfloat16, FWD>(p.out, st);
 }
 // a [M][KD] (lda), w [2F][K] (ldw): rows TMA can address
-// signal: NULL, or what the launch is to compute dz from first; counters: one for the rows handed out, then one a row of tiles
-int gated_tensor(bool fwd, const void* a, long lda, const void* w, long ldw, int M, int K, int F, GatedOut out, int* status, cudaStream_t st,
-                 const GatedSignal* signal = nullptr, int* counters = nullptr) {
+int gated_tensor(bool fwd, const void* a, long lda, const void* w, long ldw, int M, int K, int F, GatedOut out, int* status, cudaStream_t st) {
     using namespace tc::gt;
     const int KD = fwd ? K : 2 * F, cols = fwd ? F : K;
     const GatedCut cut = gated_cut(M, cols, KD, fwd, false);
@@ -404,13 +391,6 @@ int gated_tensor(bool fwd, const void* a, long lda, const void* w, long ldw, int
         }
     }
     if (!ok) return DPCLIP_ERR_CUDA;
-    if (signal) {
-        p.signal = *signal;
-        p.next = counters; p.done = counters + 1;
-        p.rows_per_take = clamp_int(2048 / F, 1, 32);
-        if (cudaMemsetAsync(counters, 0, sizeof(int) * (1 + (size_t)p.tiles_m), st) != cudaSuccess) return DPCLIP_ERR_CUDA;
-        return launch_gated_tc<false, false, 128, true>(maps, p, st);
-    }
     if (!fwd) return cut.hn == 128 ? launch_gated_tc<false, false, 128>(maps, p, st) : launch_gated_tc<false, false, 64>(maps, p, st);
     if (keep) return cut.hn == 128 ? launch_gated_tc<true, true, 128>(maps, p, st) : launch_gated_tc<true, true, 64>(maps, p, st);
     return cut.hn == 128 ? launch_gated_tc<true, false, 128>(maps, p, st) : launch_gated_tc<true, false, 64>(maps, p, st);
@@ -716,12 +696,6 @@ int dpclip_gated_backward(const void* dH, long lddh, const void* Z, long ldz, co
     const long v = dtype == DPCLIP_F32 ? 4 : 8;
     const bool vec = is_aligned(dH, 16) && is_aligned(Z, 16) && is_aligned(dZ, 16) && F % v == 0 && lddh % v == 0 && ldz % v == 0 && lddz % v == 0;
     s.per_row = vec ? F / (int)v : F;
-    if (tensor && dz_ok && w_ok && vec && gated_fuse(M, K, F)) {
-        GatedOut out;
-        memset(&out, 0, sizeof(out));
-        out.h = dX; out.ldh = lddx; out.M = M; out.F = K; out.splits = 1;
-        return gated_tensor(false, dZ, lddz, W, ldw, M, K, F, out, static_cast<int*>(workspace), st, &s, reinterpret_cast<int*>(ws));
-    }
     const int tall = s.per_row < 256 ? 256 / s.per_row : 1;
     const int grid = clamp_int(((long)M + tall - 1) / tall, 1, kNumSMs * 8);
     if (dtype == DPCLIP_F32) {

@@ -76,37 +76,6 @@ template <int ACT> __device__ __forceinline__ f32x2 gate_pair(f32x2 g, f32x2 u) 
         return make_f32x2(gate_act<ACT, false>(a) * c, gate_act<ACT, false>(b) * d);
     }
 }
-// dg = dh u act'(g), du = dh act(g) of a pair, likewise
-template <int ACT> __device__ __forceinline__ void gate_pair_grad(f32x2 dh, f32x2 g, f32x2 u, f32x2& dg, f32x2& du) {
-    if constexpr (ACT == DPCLIP_ACT_SILU || ACT == DPCLIP_ACT_GELU_TANH) {
-        const f32x2 one = make_f32x2(1.f, 1.f);
-        f32x2 e, gg;
-        if constexpr (ACT == DPCLIP_ACT_SILU) e = mul2(g, make_f32x2(-kLog2e, -kLog2e));
-        else {
-            constexpr float a = -2.f * kGeluTanh * kLog2e, b = a * kGeluCube;
-            gg = mul2(g, g);
-            e = mul2(g, fma2(gg, make_f32x2(b, b), make_f32x2(a, a)));
-        }
-        float x, y;
-        split_f32x2(e, x, y);
-        split_f32x2(add2(make_f32x2(gate_ex2(x), gate_ex2(y)), one), x, y);
-        const f32x2 p = make_f32x2(gate_rcp(x), gate_rcp(y)), a = mul2(g, p);
-        f32x2 rest = sub2(one, p);
-        if constexpr (ACT == DPCLIP_ACT_GELU_TANH) {
-            constexpr float c = 2.f * kGeluTanh, d = 3.f * c * kGeluCube;
-            rest = mul2(rest, fma2(gg, make_f32x2(d, d), make_f32x2(c, c)));
-        }
-        dg = mul2(mul2(dh, u), fma2(a, rest, p));
-        du = mul2(dh, a);
-    } else {
-        float h0, h1, g0, g1, u0, u1, a0, a1, s0, s1;
-        split_f32x2(dh, h0, h1); split_f32x2(g, g0, g1); split_f32x2(u, u0, u1);
-        gate_act_grad<ACT, false>(g0, a0, s0);
-        gate_act_grad<ACT, false>(g1, a1, s1);
-        dg = make_f32x2(h0 * u0 * s0, h1 * u1 * s1);
-        du = make_f32x2(h0 * a0, h1 * a1);
-    }
-}
 template <bool EXACT, typename F> __device__ __forceinline__ void gate_dispatch(int act, F f) {
     switch (act) {
         case DPCLIP_ACT_SILU: f(std::integral_constant<int, DPCLIP_ACT_SILU>()); break;
@@ -186,13 +155,14 @@ gated_signal_kernel(const __grid_constant__ GatedSignal p) {
                     uint32_t a[4], b[4];
 #pragma unroll
                     for (int k = 0; k < 4; ++k) {
+                        float x0, y0;
                         if constexpr (V == 8) {
-                            f32x2 dg, du;
-                            gate_pair_grad<ACT>(bf16x2_to_f32x2(hw[k]), bf16x2_to_f32x2(gw[k]), bf16x2_to_f32x2(uw[k]), dg, du);
-                            a[k] = f32x2_to_bf16x2(dg);
-                            b[k] = f32x2_to_bf16x2(du);
+                            float x1, y1;
+                            one(__uint_as_float(hw[k] << 16), __uint_as_float(gw[k] << 16), __uint_as_float(uw[k] << 16), x0, y0);
+                            one(__uint_as_float(hw[k] & 0xFFFF0000u), __uint_as_float(gw[k] & 0xFFFF0000u), __uint_as_float(uw[k] & 0xFFFF0000u), x1, y1);
+                            a[k] = f32x2_to_bf16x2(make_f32x2(x0, x1));
+                            b[k] = f32x2_to_bf16x2(make_f32x2(y0, y1));
                         } else {
-                            float x0, y0;
                             one(__uint_as_float(hw[k]), __uint_as_float(gw[k]), __uint_as_float(uw[k]), x0, y0);
                             a[k] = __float_as_uint(x0); b[k] = __float_as_uint(y0);
                         }
@@ -483,9 +453,8 @@ constexpr int BOX_BYTES = 32 * 128;                      // 32 rows x 64 bf16 of
 // Epilogue warps and the boxes of outputs they stage.  Forward: 16 warps, each 32 rows x 32 columns of h (and of zg, zu); two neighbours fill a
 // box together.  (With 8 warps of 64 columns the epilogue's latency, not its 0.24 of the issue slots, paced the kernel: 133 us.)  Backward: 8
 // warps, each 32 rows x HN columns of dx.
-// FUSE (backward): twelve more warps compute dz, see below.
-template <bool FWD, bool KEEP, int HN, bool FUSE = false> struct Cfg {
-    static constexpr int EPI_WARPS = FWD ? 16 : 8, SIGNAL_WARPS = FUSE ? 12 : 0, THREADS = 64 + 32 * (EPI_WARPS + SIGNAL_WARPS);
+template <bool FWD, bool KEEP, int HN> struct Cfg {
+    static constexpr int EPI_WARPS = FWD ? 16 : 8, THREADS = 64 + 32 * EPI_WARPS;
     static constexpr int BOXES = FWD ? (KEEP ? 3 : 1) : HN / 64;         // of a pair of warps, or of a warp
     static constexpr int STAGE_BYTES = A_BYTES + HN * 128;
     static constexpr int STAGING = 8 * BOXES * BOX_BYTES;
@@ -500,9 +469,6 @@ struct Params {
     int tma_out;                         // outputs go by TMA; else by plain stores
     int* status;
     GatedOut out;
-    GatedSignal signal;                  // FUSE
-    int* next; int* done;                // FUSE: groups of rows handed out; rows of dz that are written, by row of tiles
-    int rows_per_take;
 };
 // Tiles in groups of eight rows of tiles, along the rows first: 74 pairs then work on an 8 x 9 block of the product, whose operands stay in L2.
 struct Tile { int m, n, split; };
@@ -528,23 +494,6 @@ __device__ __forceinline__ void tma_store_2d(const CUtensorMap* map, const void*
     asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%2, %3}], [%1];"
                  ::"l"(reinterpret_cast<uint64_t>(map)), "r"(smem_u32(smem_src)), "r"(x), "r"(y) : "memory");
 }
-__device__ __forceinline__ void add_release(int* p, int v) { asm volatile("red.release.gpu.global.add.s32 [%0], %1;" ::"l"(p), "r"(v) : "memory"); }
-// Wait, bounded as mbar_wait is, until *count has reached `rows`.
-__device__ __forceinline__ bool wait_rows(const int* count, int rows, volatile int* abort_flag, int* status) {
-    const uint64_t t0 = global_ns();
-    while (true) {
-        int v;
-        asm volatile("ld.acquire.gpu.global.s32 %0, [%1];" : "=r"(v) : "l"(count) : "memory");
-        if (v >= rows) return true;
-        if (*abort_flag) return false;
-        if (global_ns() - t0 > kWaitLimitNs) {
-            *abort_flag = 1;
-            if (status) atomicExch(status, (int)DPCLIP_ERR_TIMEOUT);
-            return false;
-        }
-        __nanosleep(100);
-    }
-}
 __device__ __forceinline__ void bulk_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
 __device__ __forceinline__ void bulk_wait_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
 __device__ __forceinline__ void bulk_wait() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
@@ -553,16 +502,11 @@ __device__ __forceinline__ void bulk_wait() { asm volatile("cp.async.bulk.wait_g
 // Warp 0: loads of this CTA's operands (A rows; gate or up rows of W, or half of the columns of W), all counted on CTA 0's `full`; warp 1 of
 // CTA 0: MMAs, commits to both CTAs' `empty` and `acc_full`; the others: epilogue, warp w on lanes 32 (w % 4) .. + 31 of the tensor memory.
 // The accumulator is double-buffered (2 x 2 HN <= 512 columns), so a tile's epilogue runs under the next tile's MMAs.  Every wait is bounded.
-//
-// FUSE: dz is computed here too, by warps of their own, while the tiles of rows that are done are multiplied: the one is bound by memory, the
-// other by the tensor cores.  The signal warps take groups of rows in order from a counter, and a row of tiles is loaded when all its rows have
-// been counted as written.  Nobody waits for a CTA that may not run yet: whoever has taken rows is running and waits for nothing.  The writes
-// are generic, the loads are the async proxy's: the proxies are fenced on both sides of the counter.
-template <bool FWD, bool KEEP, int HN, bool FUSE>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__((gt::Cfg<FWD, KEEP, HN, FUSE>::THREADS), 1)
+template <bool FWD, bool KEEP, int HN>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__((gt::Cfg<FWD, KEEP, HN>::THREADS), 1)
 gated_tc_kernel(const __grid_constant__ gt::Maps maps, const __grid_constant__ gt::Params p) {
     using namespace gt;
-    using C = Cfg<FWD, KEEP, HN, FUSE>;
+    using C = Cfg<FWD, KEEP, HN>;
     constexpr int STAGES = C::STAGES, STAGE_BYTES = C::STAGE_BYTES, N = 2 * HN;
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);     // the same offset in both CTAs
@@ -600,11 +544,6 @@ gated_tc_kernel(const __grid_constant__ gt::Maps maps, const __grid_constant__ g
                 const Tile w = tile_at(p, t);
                 const int kb0 = w.split * p.kb_per_split, kb1 = min(p.KB, kb0 + p.kb_per_split);
                 const int m0 = w.m * 2 * BM_CTA + (int)rank * BM_CTA;
-                if constexpr (FUSE) {
-                    ok = wait_rows(p.done + w.m, min(2 * BM_CTA, p.out.M - w.m * 2 * BM_CTA), abort_flag, p.status);
-                    if (!ok) break;
-                    asm volatile("fence.proxy.async.global;" ::: "memory");
-                }
                 for (int kb = kb0; kb < kb1; ++kb) {
                     ok = mbar_wait(&empty[stage], phase ^ 1, abort_flag, p.status);
                     if (!ok) break;
@@ -751,49 +690,6 @@ gated_tc_kernel(const __grid_constant__ gt::Maps maps, const __grid_constant__ g
             }
         }
         if (stores) bulk_wait();
-    } else if (FUSE && warp >= 2 + C::EPI_WARPS) {
-        // ------------------------------------------------ dz of the rows this warp takes
-        const GatedSignal& s = p.signal;
-        gate_dispatch<false>(s.act, [&](auto act) {
-            constexpr int ACT = decltype(act)::value;
-            while (true) {
-                int take = 0;
-                if (lane == 0) take = atomicAdd(p.next, 1);
-                const long m_begin = (long)__shfl_sync(0xFFFFFFFFu, take, 0) * p.rows_per_take;
-                if (m_begin >= s.M) break;
-                const long m_end = min(m_begin + p.rows_per_take, s.M);
-                for (long m = m_begin; m < m_end; ++m) {
-                    const __nv_bfloat16* const dh = static_cast<const __nv_bfloat16*>(s.dh) + m * s.lddh;
-                    const __nv_bfloat16* const z = static_cast<const __nv_bfloat16*>(s.z) + m * s.ldz;
-                    __nv_bfloat16* const dz = static_cast<__nv_bfloat16*>(s.dz) + m * s.lddz;
-#pragma unroll 2
-                    for (int f = lane * 8; f < s.F; f += 256) {
-                        const uint4 h = __ldcs(reinterpret_cast<const uint4*>(dh + f)), g = __ldcs(reinterpret_cast<const uint4*>(z + f)),
-                                    u = __ldcs(reinterpret_cast<const uint4*>(z + s.F + f));
-                        const uint32_t hw[4] = {h.x, h.y, h.z, h.w}, gw[4] = {g.x, g.y, g.z, g.w}, uw[4] = {u.x, u.y, u.z, u.w};
-                        uint32_t a[4], b[4];
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) {
-                            f32x2 dg, du;
-                            gate_pair_grad<ACT>(bf16x2_to_f32x2(hw[k]), bf16x2_to_f32x2(gw[k]), bf16x2_to_f32x2(uw[k]), dg, du);
-                            a[k] = f32x2_to_bf16x2(dg);
-                            b[k] = f32x2_to_bf16x2(du);
-                        }
-                        *reinterpret_cast<uint4*>(dz + f) = make_uint4(a[0], a[1], a[2], a[3]);
-                        *reinterpret_cast<uint4*>(dz + s.F + f) = make_uint4(b[0], b[1], b[2], b[3]);
-                    }
-                }
-                asm volatile("fence.proxy.async.global;" ::: "memory");
-                __threadfence();
-                __syncwarp();
-                if (lane == 0) {
-                    // a group of rows may end in the next row of tiles
-                    const long cut = min(m_end, (m_begin / (2 * BM_CTA) + 1) * (2 * BM_CTA));
-                    add_release(p.done + m_begin / (2 * BM_CTA), (int)(cut - m_begin));
-                    if (cut < m_end) add_release(p.done + cut / (2 * BM_CTA), (int)(m_end - cut));
-                }
-            }
-        });
     } else {
         // ------------------------------------------------ epilogue, backward: HN columns a warp
         const int quarter = warp & 3, half = (warp - 2) >> 2;
