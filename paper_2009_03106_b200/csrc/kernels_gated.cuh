@@ -76,6 +76,37 @@ template <int ACT> __device__ __forceinline__ f32x2 gate_pair(f32x2 g, f32x2 u) 
         return make_f32x2(gate_act<ACT, false>(a) * c, gate_act<ACT, false>(b) * d);
     }
 }
+// dg = dh u act'(g), du = dh act(g) of a pair, likewise
+template <int ACT> __device__ __forceinline__ void gate_pair_grad(f32x2 dh, f32x2 g, f32x2 u, f32x2& dg, f32x2& du) {
+    if constexpr (ACT == DPCLIP_ACT_SILU || ACT == DPCLIP_ACT_GELU_TANH) {
+        const f32x2 one = make_f32x2(1.f, 1.f);
+        f32x2 e, gg;
+        if constexpr (ACT == DPCLIP_ACT_SILU) e = mul2(g, make_f32x2(-kLog2e, -kLog2e));
+        else {
+            constexpr float a = -2.f * kGeluTanh * kLog2e, b = a * kGeluCube;
+            gg = mul2(g, g);
+            e = mul2(g, fma2(gg, make_f32x2(b, b), make_f32x2(a, a)));
+        }
+        float x, y;
+        split_f32x2(e, x, y);
+        split_f32x2(add2(make_f32x2(gate_ex2(x), gate_ex2(y)), one), x, y);
+        const f32x2 p = make_f32x2(gate_rcp(x), gate_rcp(y)), a = mul2(g, p);
+        f32x2 rest = sub2(one, p);
+        if constexpr (ACT == DPCLIP_ACT_GELU_TANH) {
+            constexpr float c = 2.f * kGeluTanh, d = 3.f * c * kGeluCube;
+            rest = mul2(rest, fma2(gg, make_f32x2(d, d), make_f32x2(c, c)));
+        }
+        dg = mul2(mul2(dh, u), fma2(a, rest, p));
+        du = mul2(dh, a);
+    } else {
+        float h0, h1, g0, g1, u0, u1, a0, a1, s0, s1;
+        split_f32x2(dh, h0, h1); split_f32x2(g, g0, g1); split_f32x2(u, u0, u1);
+        gate_act_grad<ACT, false>(g0, a0, s0);
+        gate_act_grad<ACT, false>(g1, a1, s1);
+        dg = make_f32x2(h0 * u0 * s0, h1 * u1 * s1);
+        du = make_f32x2(h0 * a0, h1 * a1);
+    }
+}
 template <bool EXACT, typename F> __device__ __forceinline__ void gate_dispatch(int act, F f) {
     switch (act) {
         case DPCLIP_ACT_SILU: f(std::integral_constant<int, DPCLIP_ACT_SILU>()); break;
@@ -155,14 +186,13 @@ gated_signal_kernel(const __grid_constant__ GatedSignal p) {
                     uint32_t a[4], b[4];
 #pragma unroll
                     for (int k = 0; k < 4; ++k) {
-                        float x0, y0;
                         if constexpr (V == 8) {
-                            float x1, y1;
-                            one(__uint_as_float(hw[k] << 16), __uint_as_float(gw[k] << 16), __uint_as_float(uw[k] << 16), x0, y0);
-                            one(__uint_as_float(hw[k] & 0xFFFF0000u), __uint_as_float(gw[k] & 0xFFFF0000u), __uint_as_float(uw[k] & 0xFFFF0000u), x1, y1);
-                            a[k] = f32x2_to_bf16x2(make_f32x2(x0, x1));
-                            b[k] = f32x2_to_bf16x2(make_f32x2(y0, y1));
+                            f32x2 dg, du;
+                            gate_pair_grad<ACT>(bf16x2_to_f32x2(hw[k]), bf16x2_to_f32x2(gw[k]), bf16x2_to_f32x2(uw[k]), dg, du);
+                            a[k] = f32x2_to_bf16x2(dg);
+                            b[k] = f32x2_to_bf16x2(du);
                         } else {
+                            float x0, y0;
                             one(__uint_as_float(hw[k]), __uint_as_float(gw[k]), __uint_as_float(uw[k]), x0, y0);
                             a[k] = __float_as_uint(x0); b[k] = __float_as_uint(y0);
                         }

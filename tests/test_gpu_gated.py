@@ -278,3 +278,57 @@ def test_fp32_products_in_planes(dp, shape, layout, with_bias):
     dp.dpclip_gated_forward(rows(X, layout, F32), dev[1], None, H, Z, dp.DPCLIP_ACT_GELU, ws)
     bad = ~torch.isfinite(Z)
     assert bool(bad[3].all()) and bool(bad[7].all()) and not bool(bad[8].any()) and not bool(bad[2].any())
+
+
+@pytest.mark.parametrize("M,K,F,act,in_place", [(9473, 1024, 1800, "silu", False), (9728, 1000, 2048, "gelu_tanh", True), (40000, 256, 424, "gelu", False),
+                                                (38000, 264, 520, "relu", True)])
+def test_backward_large(dp, M, K, F, act, in_place):
+    """Many tiles: every row of both outputs, twice, and as a recorded graph on a stream of its own with other inputs in the same
+    buffers."""
+    g = torch.Generator(device="cuda").manual_seed(M)
+    Z = (2 * torch.randn((M, 2 * F), generator=g, device="cuda")).bfloat16()
+    dH, W = torch.randn((M, F), generator=g, device="cuda").bfloat16(), (torch.randn((2 * F, K), generator=g, device="cuda") / math.sqrt(K)).bfloat16()
+    dZ, check_z = guarded((M, 2 * F), BF16)
+    dX, check_x = guarded((M, K), BF16)
+    ws = workspace(dp, dp.dpclip_gated_workspace_bytes(M, K, F, 1))
+    run = lambda: dp.dpclip_gated_backward(dH, dZ if in_place else Z, W, dZ, dX, code(dp, act), ws)        # noqa: E731
+
+    def verify():
+        check_z(); check_x()
+        for r in range(0, M, 4096):                                # in pieces: 64 bits of everything would be several GB
+            z, dh = Z[r:r + 4096].double(), dH[r:r + 4096].double()
+            zg, zu = z[:, :F], z[:, F:]
+            a, slope = act_and_slope(zg, act)
+            want = torch.cat([dh * zu * slope, dh * a], 1)
+            off = torch.cat([fast(BF16, zg) * (dh * zu).abs(), fast(BF16, zg) * (dh * zg).abs()], 1)
+            got = dZ[r:r + 4096].double()
+            close(got, want.cpu(), (HALF_STEP[BF16] * 1.01 * want.abs() + off + 1e-37).cpu())
+            dx = got @ W.double()
+            close(dX[r:r + 4096], dx.cpu(), (HALF_STEP[BF16] * dx.abs() * 1.01 + 2 * (2 * F + 2) * U32 * (got.abs() @ W.double().abs())).cpu())
+
+    if in_place:
+        dZ.copy_(Z)
+    run()
+    torch.cuda.synchronize()
+    assert dp.dpclip_read_status(ws) == 0
+    verify()
+    first, first_x = dZ.clone(), dX.clone()
+    dX.fill_(0.5)
+    if in_place:
+        dZ.copy_(Z)
+    run()
+    assert torch.equal(first, dZ) and torch.equal(first_x, dX)
+    graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    if in_place:
+        dZ.copy_(Z)
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.graph(graph, stream=side):
+        run()
+    dH.mul_(-0.5)
+    for _ in range(2):
+        if in_place:
+            dZ.copy_(Z)
+        graph.replay()
+    torch.cuda.synchronize()
+    verify()
+    assert torch.equal(dX, first_x * -0.5) and dp.dpclip_read_status(ws) == 0
