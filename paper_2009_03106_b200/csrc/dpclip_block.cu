@@ -471,8 +471,22 @@ int dpclip_stored_clipped_grad(const float* grads, long ld, int B, int n, const 
     p.G = grads; p.ld = ld; p.B = B; p.n = n; p.clip = clip; p.g = g; p.noise_scale = sigma * C;
     p.k0 = (uint32_t)seed; p.k1 = (uint32_t)(seed >> 32); p.s0 = (uint32_t)stream_id; p.s1 = (uint32_t)(stream_id >> 32);
     cudaStream_t st = (cudaStream_t)stream;
-    return B > 64 ? launch_after(stored_grad_kernel<32>, dim3(ceil_div(n, 32)), 1024, 0, st, p)
-                   : launch_after(stored_grad_kernel<8>, dim3(ceil_div(n, 32)), 256, 0, st, p);
+    const int blocks = ceil_div(n, 32);
+    if (B <= 64) return launch_after(stored_grad_kernel<8, false>, dim3(blocks), 256, 0, st, p);
+    if (B <= STORED_PER_CTA || blocks >= kNumSMs) return launch_after(stored_grad_kernel<32, false>, dim3(blocks), 1024, 0, st, p);
+    p.cluster = 2;
+    while (p.cluster < STORED_MAX_CLUSTER && p.cluster * STORED_PER_CTA < B) p.cluster *= 2;
+    cudaLaunchConfig_t cfg;
+    memset(&cfg, 0, sizeof(cfg));
+    cfg.gridDim = dim3(blocks * p.cluster); cfg.blockDim = dim3(1024); cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = p.cluster; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr; cfg.numAttrs = overlap_allowed() ? 2 : 1;
+    if (cudaLaunchKernelEx(&cfg, stored_grad_kernel<32, true>, p) != cudaSuccess) { cudaGetLastError(); return DPCLIP_ERR_CUDA; }
+    return finish_launch();
 }
 
 int dpclip_relbias_bucket(const dpclip_relbias* config, long distance) {
@@ -599,13 +613,17 @@ int dpclip_qknorm_backward(const dpclip_heads* parts, int n_parts, int B, int T,
     if (rc) return rc;
     QkFinish f;
     memset(&f, 0, sizeof(f));
-    f.D = D;
+    f.D = D; f.B = B;
     bool any = false;
     for (int k = 0; k < n_parts; ++k) {
-        f.part[k] = p.part[k].part; f.chunks[k] = (int)sums[k]; f.grads[k] = grads[k]; f.sq[k] = sq_layers[k];
+        f.part[k] = p.part[k].part; f.sums[k] = (int)sums[k]; f.grads[k] = grads[k]; f.sq[k] = sq_layers[k];
         any = any || grads[k] || sq_layers[k];
     }
-    return any ? launch_after(qknorm_finish_kernel, dim3(B, n_parts), QK_THREADS, 0, st, f) : DPCLIP_OK;
+    if (!any) return DPCLIP_OK;
+    // about two warps an SM's scheduler are enough: beyond that a CTA an example only queues
+    if (B > 8 * kNumSMs && sums[0] <= 8 && sums[1] <= 8)
+        return launch_after(qknorm_finish_kernel<true>, dim3(ceil_div(B, QK_THREADS / 32), n_parts), QK_THREADS, 0, st, f);
+    return launch_after(qknorm_finish_kernel<false>, dim3(B, n_parts), QK_THREADS, 0, st, f);
 }
 
 size_t dpclip_gated_workspace_bytes(int M, int K, int F, dpclip_dtype dtype) {

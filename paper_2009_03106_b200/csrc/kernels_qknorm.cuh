@@ -660,25 +660,30 @@ qknorm_backward_ring_kernel(const __grid_constant__ QkParams p) {
     }
 }
 
-// grads[i][d] = the chunks' sums in order, sq[i] = the sum of their squares; blockIdx.y = queries, keys.
-struct QkFinish { const float* part[2]; int chunks[2]; float* grads[2]; float* sq[2]; int D; };
+// grads[i][d] = the partial sums in order, sq[i] = the sum of their squares; blockIdx.y = queries, keys.  A CTA an example, or, where the
+// examples are many and their partial sums few, a warp.
+struct QkFinish { const float* part[2]; int sums[2]; float* grads[2]; float* sq[2]; int B, D; };
+template <bool WARP>
 __global__ void __launch_bounds__(QK_THREADS)
 qknorm_finish_kernel(const __grid_constant__ QkFinish p) {
     __shared__ float red[32];
     griddep_wait();
     griddep_launch_dependents();
-    const int i = blockIdx.x, which = blockIdx.y, chunks = p.chunks[which];
+    const int i = WARP ? (int)blockIdx.x * (QK_THREADS / 32) + (int)(threadIdx.x >> 5) : (int)blockIdx.x, which = blockIdx.y, sums = p.sums[which];
+    if (i >= p.B) return;
+    const int first = WARP ? threadIdx.x & 31 : threadIdx.x, step = WARP ? 32 : QK_THREADS;
     float total = 0.f;
-    for (int d = threadIdx.x; d < p.D; d += QK_THREADS) {
-        const float* src = p.part[which] + (size_t)i * chunks * p.D + d;
+    for (int d = first; d < p.D; d += step) {
+        const float* src = p.part[which] + (size_t)i * sums * p.D + d;
         float a = 0.f;
 #pragma unroll 8
-        for (int c = 0; c < chunks; ++c) a += src[(size_t)c * p.D];
+        for (int c = 0; c < sums; ++c) a += src[(size_t)c * p.D];
         if (p.grads[which]) p.grads[which][(size_t)i * p.D + d] = a;
         total = fmaf(a, a, total);
     }
-    total = block_sum(total, red);
-    if (threadIdx.x == 0 && p.sq[which]) p.sq[which][i] = total;
+    if (WARP) total = warp_sum(total);
+    else total = block_sum(total, red);
+    if (first == 0 && p.sq[which]) p.sq[which][i] = total;
 }
 
 // table[pos][0][i] = cos(pos base^(-2i / rot) / scale), table[pos][1][i] its sine: angles in 64 bits, far positions lose theirs in 32.

@@ -254,6 +254,11 @@ QK = [
     (1, 5, 1, 1, 1, 0, False),
     (2, 6, 3, 0, 64, 0, False),               # queries alone, no rotation
     (4, 260, 16, 2, 128, 128, True),
+    (1300, 1, 2, 1, 32, 32, False),           # many examples of one token
+    (1250, 3, 1, 2, 50, 20, True),
+    (2, 700, 20, 3, 80, 80, False),           # rings of copies, head blocks that are not full, idle lanes
+    (3, 300, 7, 5, 160, 96, True),
+    (40, 64, 9, 0, 32, 32, False),
 ]
 
 
@@ -469,7 +474,7 @@ def test_default_positions_and_far_angles(dp):
 # ---------------------------------------------------------------------------------------------------------------
 # clipped sums of stored gradients
 # ---------------------------------------------------------------------------------------------------------------
-@pytest.mark.parametrize("B,n", [(1, 1), (7, 33), (128, 512), (257, 100), (5000, 31)])
+@pytest.mark.parametrize("B,n", [(1, 1), (7, 33), (128, 512), (257, 100), (5000, 31), (700, 33), (1025, 64), (600, 5000)])
 @pytest.mark.parametrize("with_clip", [True, False])
 def test_stored_clipped_grad(dp, B, n, with_clip):
     g = torch.Generator().manual_seed(B * n)
