@@ -56,7 +56,7 @@ bool fill_buckets(RbBuckets& r, const dpclip_relbias* c) {
 }
 
 // A tile of the gradient: G groups of nr block rows by KT block columns.  64 threads where the rows have at most 64 blocks: a walk of such a
-// tile is then long enough to pay for the folds behind it (128 examples, 8 heads, 256 x 256, bf16: XX us, 256 threads YY).
+// tile is then long enough to pay for the folds behind it (128 examples, 8 heads, 256 x 256, bf16: 40 us, 256 threads 48).
 struct RbTiles { int E, threads, nqb, nkb, KT, G, nr, qtiles, ktiles; };
 RbTiles relbias_tiles(int B, int H, int Tq, int Tk, bool blocks8) {
     RbTiles t;
@@ -69,15 +69,15 @@ RbTiles relbias_tiles(int B, int H, int Tq, int Tk, bool blocks8) {
     t.G = t.threads / t.KT;
     if (t.G < 1) t.G = 1;
     if (t.G > t.nqb) t.G = t.nqb;
-    // long walks, as long as there are CTAs enough for every SM and 40 KB of shared memory hold the sums
+    // One wave of the CTAs that fit on the SMs side by side, their walks as long as that allows: a walk's end costs as much as eight blocks of
+    // it.  40 KB of shared memory hold the sums; walks over single elements are at least eight long.
+    const long resident = (long)kNumSMs * (blocks8 ? 512 : 1024) / t.threads, planes = (long)B * H * t.ktiles;
+    const long rows = resident / planes > 0 ? resident / planes : 1;
     const int longest = blocks8 ? 32 : 128;
-    const long ctas = t.threads == RB_THREADS ? 4L * kNumSMs : 12L * kNumSMs;
-    t.nr = 1;
     auto fits = [&](int nr) { return (blocks8 ? rb_smem_floats<8>(t.KT, t.G, nr) : rb_smem_floats<1>(t.KT, t.G, nr)) * sizeof(float) <= 40 * 1024; };
-    while (t.nr < longest && t.G * t.nr < t.nqb && fits(2 * t.nr) &&
-           ((long)t.ktiles * ceil_div(t.nqb, (long)t.G * t.nr * 2) * B * H >= ctas || (long)B * H * 2 >= ctas)) t.nr *= 2;
-    // rows of single elements are walked eight at a time at least: fewer would be all set-up
-    if (!blocks8) while (t.nr < 8 && t.G * t.nr < t.nqb) t.nr *= 2;
+    t.nr = clamp_int(ceil_div(t.nqb, t.G * rows), 1, longest);
+    if (!blocks8 && t.nr < 8) t.nr = 8;
+    while (t.nr > 1 && !fits(t.nr)) t.nr = (t.nr + 1) / 2;
     t.qtiles = ceil_div(t.nqb, (long)t.G * t.nr);
     return t;
 }
