@@ -68,7 +68,7 @@ template <int ACT> __device__ __forceinline__ f32x2 gate_pair(f32x2 g, f32x2 u) 
         float x, y;
         split_f32x2(e, x, y);
         split_f32x2(add2(make_f32x2(gate_ex2(x), gate_ex2(y)), make_f32x2(1.f, 1.f)), x, y);
-        return mul2(mul2(g, u), make_f32x2(gate_rcp(x), gate_rcp(y)));
+        return mul2(mul2(g, make_f32x2(gate_rcp(x), gate_rcp(y))), u);      // act first: g u may overflow where act(g) is zero
     } else {
         float a, b, c, d;
         split_f32x2(g, a, b);
@@ -631,29 +631,31 @@ gated_tc_kernel(const __grid_constant__ gt::Maps maps, const __grid_constant__ g
         const uint32_t acc_empty0 = mapa_shared(smem_u32(acc_empty), 0);
         const GatedOut& o = p.out;
         int it = 0;
+        bool ok = true;
         for (int t = pair; t < p.total; t += pairs, ++it) {
             const Tile w = tile_at(p, t);
             const int buf = it & 1;
             const int row0 = w.m * 2 * BM_CTA + (int)rank * BM_CTA + quarter * 32;
             const int box_col = w.n * HN + box * 64, col = box_col + (group & 1) * 32;
-            if (!mbar_wait(&acc_full[buf], (it >> 1) & 1, abort_flag, p.status)) break;
+            // A wait that ran out must not leave the box's other warp at a barrier: from then on both only keep step.
+            ok = __all_sync(0xFFFFFFFFu, ok && mbar_wait(&acc_full[buf], (it >> 1) & 1, abort_flag, p.status));
             tc_fence_after_sync();
             const uint32_t tm = tmem_base + ((uint32_t)(quarter * 32) << 16) + buf * N + group * 32;
             const bool there = group * 32 < HN && row0 < o.M && box_col < o.F;   // the same for both warps of a box
             uint32_t g[32], u[32];
-            if (there) {
+            if (there && ok) {
                 tmem_ld_32x32(tm, g);
                 tmem_ld_32x32(tm + HN, u);
                 tmem_ld_wait();
             }
             tc_fence_before_sync();
             __syncwarp();
-            if (lane == 0) mbar_arrive_cluster(acc_empty0 + buf * 8);
+            if (lane == 0 && ok) mbar_arrive_cluster(acc_empty0 + buf * 8);
             if (!there) continue;
             if (o.splits > 1) {
                 // partial products: a thread's row, 128 bytes of it
                 const int m = row0 + lane;
-                if (m < o.M) {
+                if (m < o.M && ok) {
                     float* to = o.part + ((long)w.split * o.M + m) * 2L * o.F + col;
 #pragma unroll
                     for (int j = 0; j < 32; ++j)
@@ -663,6 +665,10 @@ gated_tc_kernel(const __grid_constant__ gt::Maps maps, const __grid_constant__ g
             }
             if (stores) bulk_wait_read();                                    // the box's last tile has left
             asm volatile("bar.sync %0, 64;" ::"r"(pair_bar) : "memory");
+            if (!ok) {
+                asm volatile("bar.sync %0, 64;" ::"r"(pair_bar) : "memory");
+                continue;
+            }
             // 32 columns of a row = four 16-byte slots of a 128-byte row, at their swizzled places
             uint8_t* const mine = boxes + lane * 128;
             const int sw = lane & 7;
@@ -732,7 +738,7 @@ gated_tc_kernel(const __grid_constant__ gt::Maps maps, const __grid_constant__ g
             const int buf = it & 1;
             const int row0 = w.m * 2 * BM_CTA + (int)rank * BM_CTA + quarter * 32;
             const int col0 = w.n * N + half * HN;
-            if (!mbar_wait(&acc_full[buf], (it >> 1) & 1, abort_flag, p.status)) break;
+            if (!__all_sync(0xFFFFFFFFu, mbar_wait(&acc_full[buf], (it >> 1) & 1, abort_flag, p.status))) break;
             tc_fence_after_sync();
             const uint32_t tm = tmem_base + ((uint32_t)(quarter * 32) << 16) + buf * N + half * HN;
             const bool there = row0 < o.M && col0 < o.F;

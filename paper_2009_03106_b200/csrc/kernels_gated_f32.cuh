@@ -190,7 +190,7 @@ gated_tc3_kernel(const __grid_constant__ gt3::Maps maps, const __grid_constant__
             for (int j = 0; j < CW; ++j) { x[0][j] = 0.f; x[1][j] = 0.f; }
             for (int kb = kb0; kb < kb1; ++kb, ++it) {
                 const int buf = it & 1;
-                ok = mbar_wait(&acc_full[buf], (it >> 1) & 1, abort_flag, p.status);
+                ok = __all_sync(0xFFFFFFFFu, mbar_wait(&acc_full[buf], (it >> 1) & 1, abort_flag, p.status));
                 if (!ok) break;
                 tc_fence_after_sync();
                 const uint32_t tmem = tmem_base + ((uint32_t)(quarter * 32) << 16) + buf * N;

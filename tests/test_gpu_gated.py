@@ -155,6 +155,19 @@ def test_extreme_preactivations(dp, act):
         assert float((got[:, :F] - slope)[far].abs().max()) <= 1e-5 and float((got[:, F:] - a)[far].abs().max()) <= 1e-5
 
 
+@pytest.mark.parametrize("act", ACTS)
+def test_products_that_would_overflow(dp, act):
+    """act(zg) zu where zg zu leaves fp32: zero for the activations that vanish there."""
+    M, K, F = 300, 64, 64                                          # the tensor-core form
+    X = torch.zeros((M, K)); X[:, 0] = 2.0 ** 40
+    W = torch.zeros((2 * F, K)); W[:F, 0] = -2.0 ** 30; W[F:, 0] = 2.0 ** 30
+    for dtype in (BF16, F32):
+        ws = workspace(dp, dp.dpclip_gated_workspace_bytes(M, K, F, CODE[dtype]))
+        H = torch.empty((M, F), dtype=dtype, device="cuda")
+        dp.dpclip_gated_forward(X.to(dtype).cuda(), W.to(dtype).cuda(), None, H, None, code(dp, act), ws)
+        assert bool((H == 0).all())
+
+
 def test_against_differences(dp):
     """dX against directional differences of the forward pass in fp32; dW of the step against those of W."""
     B, T, K, F = 3, 7, 12, 10
