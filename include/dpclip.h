@@ -591,8 +591,9 @@ int dpclip_rotation_table(float* table, long n_pos, int rot_dim, double base, do
  *   X  [M][K] row stride ldx;  W [2F][K] row stride ldw;  bias [2F] fp32 or NULL;  H [M][F] row stride ldh, OVERWRITTEN
  *   Z  [M][2F] row stride ldz, OVERWRITTEN with the pre-activations (for the backward pass), or NULL
  * X, W, H, Z of one `dtype`; products are summed in fp32, H comes from the unrounded Z.  bf16 runs on the tensor cores (rows that are no
- * 16-byte multiples are laid out in the workspace first, or stay on the fp32 ALUs where that costs more), fp32 on the fp32 ALUs.  M from 1
- * (one token: the weights are streamed once).  Outputs may not overlap inputs.
+ * 16-byte multiples are laid out in the workspace first, or stay on the fp32 ALUs where that costs more).  M from 1
+ * (one token: the weights are streamed once).  Outputs may not overlap inputs.  Large fp32 calls run on the tensor cores as six products of
+ * three bf16 planes (fp32 accuracy; an infinity among the inputs can come out as NaN).
  *   workspace >= dpclip_gated_workspace_bytes(), its header set up by dpclip_workspace_init
  * Errors: INVALID_ARG, MISALIGNED, WORKSPACE. */
 typedef enum { DPCLIP_ACT_SILU = 0, DPCLIP_ACT_GELU = 1, DPCLIP_ACT_GELU_TANH = 2, DPCLIP_ACT_RELU = 3 } dpclip_activation;
