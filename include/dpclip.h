@@ -21,6 +21,8 @@
  * weight matrix, to global memory.  The 2 d numbers of an example's gradient of
  * an element-wise layer do go through the workspace in dpclip_model_step* (see
  * there); the workspace keeps them until a later call overwrites them.
+ * The transformer-block calls that return per-example gradients (of a few
+ * hundred numbers) write them to a buffer the caller gives.
  *
  * Conventions for every entry point
  *   - Pointers are DEVICE pointers unless the parameter comment says "host".

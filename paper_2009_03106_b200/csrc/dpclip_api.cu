@@ -1685,7 +1685,6 @@ namespace dpclip {
 int finish_launch() { return launch_status(); }
 bool overlap_allowed() { return !path_switch(SW_NO_OVERLAP); }
 bool tensor_cores_allowed() { return !path_switch(SW_FORCE_SIMT); }
-void log_line(const char* text) { DPCLIP_LOGF("%s", text); }
 bool encode_map_bf16(CUtensorMap* map, const void* base, long rows, long cols, long ld, int box_cols, int box_rows) {
     return make_map_bf16(map, base, rows, cols, ld, box_cols, box_rows);
 }

@@ -160,7 +160,7 @@ int launch_qk_forward(QkParams& p, cudaStream_t st) {
         }
     }
     const dim3 grid((unsigned)((tokens + WARPS - 1) / WARPS), (unsigned)blocks);
-    qknorm_forward_kernel<T, V, NCH, G, 1><<<grid, QK_THREADS, 0, st>>>(p);
+    qknorm_forward_kernel<T, V, NCH, G><<<grid, QK_THREADS, 0, st>>>(p);
     return finish_launch();
 }
 // Whether the backward pass of this shape keeps a ring of copies (its CTAs then have a block of heads each).
@@ -201,8 +201,7 @@ int launch_qk(QkParams& p, const QkShape& s, bool backward, bool ring, cudaStrea
 #undef DPCLIP_QK
 }
 
-// Chunks of positions a block of heads is cut into: about four CTAs an SM in all (two where a ring of copies is kept), at least `least`
-// positions each.
+// Chunks of positions a block of heads is cut into: about four CTAs an SM in all, at least `least` positions each.
 inline int qk_chunks(int B, int T, int blocks, bool ring) {
     const int least = ring ? 64 : 16;
     return clamp_int(4L * kNumSMs / ((long)B * blocks), 1, T / least > 0 ? T / least : 1);

@@ -10,7 +10,6 @@ namespace dpclip {
 int finish_launch();                 // counts a launch; DPCLIP_OK or DPCLIP_ERR_CUDA
 bool overlap_allowed();              // DPCLIP_NO_OVERLAP is not set
 bool tensor_cores_allowed();         // DPCLIP_FORCE_SIMT is not set
-void log_line(const char* text);     // DPCLIP_LOG=1
 // 2-D bf16 matrix [rows][cols], row stride ld elements (a multiple of 8), base 16-byte aligned; box_cols x box_rows boxes, 128-byte
 // swizzle, zeros outside
 bool encode_map_bf16(CUtensorMap* map, const void* base, long rows, long cols, long ld, int box_cols, int box_rows);

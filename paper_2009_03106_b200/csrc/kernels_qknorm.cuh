@@ -8,10 +8,11 @@
 // both members: V elements of the first half and the V of the second half that go with them (V = 16 bytes), or 2V neighbours where pairs
 // are neighbours and where nothing is rotated.  No value crosses lanes but for the sums over the head.  The groups of a warp take
 // neighbouring heads of one token, so a warp instruction covers a run of memory and all its groups read the same angles.  Heads whose
-// width or alignment does not allow that take V = 1: one warp a head, NCH pairs a lane.
+// width or alignment does not allow that take V = 1: NCH pairs a lane, one element at a time.
 //
-// Bound: memory, every input is read once and every output written once.  A warp has U heads in flight per group.  The backward pass
-// computes rms(x) again from the x it reads anyway, so the forward pass stores nothing for it.
+// Bound: memory in long calls (every input is read once, every output written once), round trips in short ones.  The backward pass computes
+// rms(x) again from the x it reads anyway, so the forward pass stores nothing for it.  128 x 256 tokens in bf16: 8 + 8 heads of 64 in 30 us (134
+// MB, what a copy takes), backward 16 + 2 heads of 128 in 113 us (453 MB).
 #pragma once
 #include "common.cuh"
 
@@ -22,8 +23,8 @@ struct QkPart {
     const void* dy; long yb, yt, yh;     // backward: the signal at the output
     void* y; long ob, ot, oh;            // forward: the output; backward: dx
     const float* gain;                   // [D] or NULL (ones)
-    float* part;                         // backward: [B][chunks][D] partial gradients
-    int H, blocks, chunks;               // head blocks (of the groups of a warp) a token; backward: CTAs an example
+    float* part;                         // backward: [B][blocks * chunks][D] partial gradients
+    int H, blocks, chunks;               // blocks of heads (those of a warp's groups) a token; backward: CTAs an example and block
 };
 struct QkParams {
     QkPart part[2];
@@ -196,8 +197,8 @@ __device__ __forceinline__ long qk_position(const QkParams& p, uint32_t token, i
 
 constexpr int QK_THREADS = 256;
 
-// blockIdx.y = block of 32 / G heads of the queries, then of the keys; a warp takes U tokens in a row of it.
-template <typename T, int V, int NCH, int G, int U>
+// blockIdx.y = block of 32 / G heads of the queries, then of the keys; a warp takes one token of it.
+template <typename T, int V, int NCH, int G>
 __global__ void __launch_bounds__(QK_THREADS)
 qknorm_forward_kernel(const __grid_constant__ QkParams p) {
     constexpr int NG = 32 / G;
@@ -205,62 +206,50 @@ qknorm_forward_kernel(const __grid_constant__ QkParams p) {
     const int which = (int)blockIdx.y >= p.part[0].blocks;
     const QkPart& y = p.part[which];
     const int h = ((int)blockIdx.y - (which ? p.part[0].blocks : 0)) * NG + grp;
-    const uint32_t tokens = (uint32_t)p.B * p.T, token0 = (blockIdx.x * (QK_THREADS / 32) + (threadIdx.x >> 5)) * U;
-    if (token0 >= tokens) return;
-    int b = (int)(token0 / p.T), t = (int)(token0 - (uint32_t)b * p.T);
+    const uint32_t tokens = (uint32_t)p.B * p.T, token = blockIdx.x * (QK_THREADS / 32) + (threadIdx.x >> 5);
+    if (token >= tokens) return;
+    const int b = (int)(token / (uint32_t)p.T), t = (int)(token - (uint32_t)b * p.T);
     const bool head = h < y.H;
+    const long pos = head ? qk_position(p, token, t) : -1;
+    const T* const x = static_cast<const T*>(y.x) + (long)b * y.xb + (long)t * y.xt + (long)h * y.xh;
+    T* const out = static_cast<T*>(y.y) + (long)b * y.ob + (long)t * y.ot + (long)h * y.oh;
     QkChunk<V> c[NCH];
-#pragma unroll
-    for (int n = 0; n < NCH; ++n) c[n].set(gl + G * n, p.D, p.rot, p.interleaved);
-    QkRaw<T, V> lo[U][NCH], hi[U][NCH];
-    long pos[U];
-    T* out[U];
-    const float inv_d = 1.f / (float)p.D;
-#pragma unroll
-    for (int k = 0; k < U; ++k) {
-        if (k > 0 && ++t == p.T) { t = 0; ++b; }
-        const bool on = head && token0 + k < tokens;
-        pos[k] = on ? qk_position(p, token0 + k, t) : -1;
-        const T* x = static_cast<const T*>(y.x) + (long)b * y.xb + (long)t * y.xt + (long)h * y.xh;
-        out[k] = static_cast<T*>(y.y) + (long)b * y.ob + (long)t * y.ot + (long)h * y.oh;
-#pragma unroll
-        for (int n = 0; n < NCH; ++n) {
-            qk_zero(lo[k][n]); qk_zero(hi[k][n]);
-            if (on && c[n].there) qk_load(x + c[n].a0, lo[k][n]);
-            if (on && c[n].second) qk_load(x + c[n].a1, hi[k][n]);
-        }
-    }
+    QkRaw<T, V> lo[NCH], hi[NCH];
     QkVec<V> gain0[NCH], gain1[NCH];
+#pragma unroll
+    for (int n = 0; n < NCH; ++n) {
+        c[n].set(gl + G * n, p.D, p.rot, p.interleaved);
+        qk_zero(lo[n]); qk_zero(hi[n]);
+        if (head && c[n].there) qk_load(x + c[n].a0, lo[n]);         // whatever the position: its load would come first
+        if (head && c[n].second) qk_load(x + c[n].a1, hi[n]);
+    }
 #pragma unroll
     for (int n = 0; n < NCH; ++n) {
         gain0[n] = qk_fill<V>(1.f); gain1[n] = qk_fill<V>(1.f);
         if (y.gain && c[n].there) gain0[n] = qk_params<V>(y.gain + c[n].a0);
         if (y.gain && c[n].second) gain1[n] = qk_params<V>(y.gain + c[n].a1);
     }
+    QkVec<V> xa[NCH], xb[NCH];
+    f32x2 ss = make_f32x2(0.f, 0.f);
 #pragma unroll
-    for (int k = 0; k < U; ++k) {
-        QkVec<V> xa[NCH], xb[NCH];
-        f32x2 ss = make_f32x2(0.f, 0.f);
+    for (int n = 0; n < NCH; ++n) {
+        xa[n] = qk_f32<T, V>(lo[n]); xb[n] = qk_f32<T, V>(hi[n]);
+        qk_dot<V>(ss, xa[n], xa[n]);
+        qk_dot<V>(ss, xb[n], xb[n]);
+    }
+    const float r = rsqrtf(fmaf(qk_group_sum<G>(sum_f32x2(ss)), 1.f / (float)p.D, p.eps));
+    if (pos < 0) return;
+    const QkVec<V> rr = qk_fill<V>(r);
 #pragma unroll
-        for (int n = 0; n < NCH; ++n) {
-            xa[n] = qk_f32<T, V>(lo[k][n]); xb[n] = qk_f32<T, V>(hi[k][n]);
-            qk_dot<V>(ss, xa[n], xa[n]);
-            qk_dot<V>(ss, xb[n], xb[n]);
+    for (int n = 0; n < NCH; ++n) {
+        xa[n] = qk_mul<V>(xa[n], qk_mul<V>(gain0[n], rr));
+        xb[n] = qk_mul<V>(xb[n], qk_mul<V>(gain1[n], rr));
+        if (c[n].turned) {
+            const float* angles = p.table + pos * p.rot + c[n].rot0;
+            qk_turn<V>(xa[n], xb[n], qk_params<V>(angles), qk_params<V>(angles + p.rot / 2), p.interleaved);
         }
-        const float r = rsqrtf(fmaf(qk_group_sum<G>(sum_f32x2(ss)), inv_d, p.eps));
-        if (pos[k] < 0) continue;
-        const QkVec<V> rr = qk_fill<V>(r);
-#pragma unroll
-        for (int n = 0; n < NCH; ++n) {
-            xa[n] = qk_mul<V>(xa[n], qk_mul<V>(gain0[n], rr));
-            xb[n] = qk_mul<V>(xb[n], qk_mul<V>(gain1[n], rr));
-            if (c[n].turned) {
-                const float* angles = p.table + pos[k] * p.rot + c[n].rot0;
-                qk_turn<V>(xa[n], xb[n], qk_params<V>(angles), qk_params<V>(angles + p.rot / 2), p.interleaved);
-            }
-            if (c[n].there) qk_store<T, V>(out[k] + c[n].a0, xa[n]);
-            if (c[n].second) qk_store<T, V>(out[k] + c[n].a1, xb[n]);
-        }
+        if (c[n].there) qk_store<T, V>(out + c[n].a0, xa[n]);
+        if (c[n].second) qk_store<T, V>(out + c[n].a1, xb[n]);
     }
 }
 
@@ -376,8 +365,8 @@ qknorm_backward_kernel(const __grid_constant__ QkParams p) {
 // ------------------------------------------------------------------------------------------------ long calls, V > 1
 // The same passes with the loads taken out of the way: every lane copies its own runs of the warp's next tokens into shared memory
 // (cp.async, 16 bytes, zero-filled where nothing is read), STAGES - 1 of them ahead, and reads back only what it copied itself, so a warp
-// waits for its own copies and for no other warp.  With loads to registers the kernels waited: 8 of 16 warps' loads were in flight at a time
-// (0.45 of the issue slots in use, 0.30 of DRAM).  Angles are loaded one token ahead.  A warp stays with one block of heads.
+// waits for its own copies and for no other warp.  With loads to registers, four heads in flight a group, the forward pass took 38 us where it
+// takes 30, the backward pass 135 (113).  A warp stays with one block of heads.
 __device__ __forceinline__ void qk_copy16(uint32_t dst, const void* src, bool on) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(on ? 16 : 0) : "memory");
 }

@@ -570,3 +570,63 @@ def test_attention_parameters_in_one_step(dp):
     graph.replay()
     torch.cuda.synchronize()
     assert torch.equal(Gt, want[2] * 0.5)
+
+
+def test_offsets_beyond_32_bits(dp):
+    """Examples that lie more than 2^31 elements apart in one buffer (a cache, a pool): read and written where they are."""
+    far = (1 << 31) + 24
+    pool = torch.empty(far + 4096, dtype=BF16, device="cuda")
+    g = torch.Generator().manual_seed(2)
+    dS = torch.randn((2, 2, 16, 24), generator=g).bfloat16()
+    dev = pool.as_strided((2, 2, 16, 24), (far, 384, 24, 1))
+    dev.copy_(dS)
+    nb = 16
+    grads, sq = torch.empty((2, nb, 2), device="cuda"), torch.empty(2, device="cuda")
+    ws = workspace(dp, dp.dpclip_relbias_workspace_bytes(2, 2, 16, 24, nb, 1))
+    dp.dpclip_relbias_sqnorms(dev, grads, sq, ws, 30)
+    want, mag = relbias_reference(dS, bucket_table(16, 24, 0, nb, 30, True), nb, False, 0, None, None)
+    close(grads, want, 700 * U32 * mag)
+    x = torch.randn((2, 3, 2, 64), generator=g).bfloat16()
+    xd = pool.as_strided((2, 3, 2, 64), (far, 128, 64, 1), 1024)
+    xd.copy_(x)
+    y = torch.empty((2, 3, 2, 64), dtype=BF16, device="cuda")
+    dp.dpclip_qknorm_forward(xd, None, None, None, None, y, None, eps=1e-5)
+    v = x.double() / torch.sqrt(x.double().square().mean(-1, keepdim=True) + 1e-5)
+    close(y, v, HALF_STEP[BF16] * v.abs() + 40 * U32 * v.abs())
+    dp.dpclip_qknorm_forward(xd, None, None, None, None, xd, None, eps=1e-5)
+    assert torch.equal(xd, y)
+
+
+def test_two_streams_at_once(dp):
+    """Calls on two streams, each with outputs and a workspace of its own, interleaved: the bits of the calls one after the other."""
+    B, T, H, D, nb = 16, 256, 8, 64, 32
+    table = torch.empty((T, 2, D // 2), device="cuda")
+    dp.dpclip_rotation_table(table)
+    sides = []
+    for k in range(2):
+        g = torch.Generator(device="cuda").manual_seed(k)
+        s = {n: torch.randn((B, T, H, D), generator=g, device="cuda").bfloat16() for n in ("q", "k", "dq", "dk")}
+        s["dS"] = torch.randn((B, H, T, T), generator=g, device="cuda").bfloat16()
+        s["ws"] = workspace(dp, max(dp.dpclip_relbias_workspace_bytes(B, H, T, T, nb, 1), dp.dpclip_qknorm_workspace_bytes(B, T, H, H, D)))
+        s["out"] = [torch.empty_like(s["q"]), torch.empty_like(s["q"]), torch.empty((B, D), device="cuda"), torch.empty((B, D), device="cuda"),
+                    torch.empty((B, nb, H), device="cuda"), torch.empty(B, device="cuda"), torch.empty((nb, H), device="cuda")]
+        s["stream"] = torch.cuda.Stream()
+        sides.append(s)
+
+    def run(s, stream):
+        o = s["out"]
+        dp.dpclip_qknorm_backward(s["dq"], s["dk"], s["q"], s["k"], None, None, table, o[0], o[1], o[2], o[3], None, None, s["ws"], stream=stream)
+        dp.dpclip_relbias_sqnorms(s["dS"], o[4], o[5], s["ws"], 128, stream=stream)
+        dp.dpclip_stored_clipped_grad(o[4], None, o[6], stream=stream)
+
+    want = []
+    for s in sides:
+        run(s, None)
+        want.append([t.clone() for t in s["out"]])
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for s in sides:
+            run(s, s["stream"])
+    torch.cuda.synchronize()
+    for s, w in zip(sides, want):
+        assert all(torch.equal(a, b) for a, b in zip(s["out"], w))

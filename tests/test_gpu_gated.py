@@ -345,3 +345,31 @@ def test_backward_large(dp, M, K, F, act, in_place):
     torch.cuda.synchronize()
     verify()
     assert torch.equal(dX, first_x * -0.5) and dp.dpclip_read_status(ws) == 0
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_two_streams_at_once(dp, dtype):
+    """Calls on two streams, each with outputs and a workspace of its own, interleaved: the bits of the calls one after the other."""
+    M, K, F = 2000, 256, 520
+    sides = []
+    for k in range(2):
+        g = torch.Generator(device="cuda").manual_seed(k)
+        X, W = torch.randn((M, K), generator=g, device="cuda").to(dtype), (torch.randn((2 * F, K), generator=g, device="cuda") / 16).to(dtype)
+        out = [torch.empty((M, n), dtype=dtype, device="cuda") for n in (F, 2 * F, 2 * F, K)]
+        sides.append((X, W, out, workspace(dp, dp.dpclip_gated_workspace_bytes(M, K, F, CODE[dtype])), torch.cuda.Stream()))
+
+    def run(X, W, out, ws, stream):
+        dp.dpclip_gated_forward(X, W, None, out[0], out[1], dp.DPCLIP_ACT_SILU, ws, stream=stream)
+        dp.dpclip_gated_backward(out[0], out[1], W, out[2], out[3], dp.DPCLIP_ACT_SILU, ws, stream=stream)
+
+    want = []
+    for s in sides:
+        run(*s[:4], None)
+        want.append([t.clone() for t in s[2]])
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for s in sides:
+            run(*s)
+    torch.cuda.synchronize()
+    for s, w in zip(sides, want):
+        assert all(torch.equal(a, b) for a, b in zip(s[2], w)) and dp.dpclip_read_status(s[3]) == 0
