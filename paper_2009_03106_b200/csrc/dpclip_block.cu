@@ -201,16 +201,28 @@ int launch_qk(QkParams& p, const QkShape& s, bool backward, bool ring, cudaStrea
 #undef DPCLIP_QK
 }
 
-// Chunks of positions a block of heads is cut into: about four CTAs an SM in all, at least `least` positions each.
-inline int qk_chunks(int B, int T, int blocks, bool ring) {
-    const int least = ring ? 64 : 16;
-    return clamp_int(4L * kNumSMs / ((long)B * blocks), 1, T / least > 0 ? T / least : 1);
+// Chunks of positions a block of heads is cut into.  Two CTAs stand on an SM; a CTA's time is about 6 us and 0.18 us a position (its eight
+// warps take one each), a call's that of its waves: the fewest chunks of the least such time.  (128 examples, five blocks of heads, 256 positions:
+// 124 us in one chunk, which is 2.2 waves, 111 in two; 4 examples, six blocks, 2000 positions: 51 us in 24 chunks, 45 in 12, which are one wave.)
+constexpr long kQkResident = 2L * kNumSMs;
+inline int qk_most_chunks(int B, int T, int blocks) {
+    const long most = 4 * kQkResident / ((long)B * blocks) + 1, least = T / 16 > 0 ? T / 16 : 1;
+    return (int)(most < least ? most : least);
 }
-// most partial sums an example any form of the kernels makes, for the workspace
+inline int qk_chunks(int B, int T, int blocks) {
+    int best = 1;
+    double least = 1e30;
+    for (int c = 1; c <= qk_most_chunks(B, T, blocks); ++c) {
+        const double time = (double)(((long)B * blocks * c + kQkResident - 1) / kQkResident) * (6.0 + 0.18 * T / c);
+        if (time < least) { least = time; best = c; }
+    }
+    return best;
+}
+// most partial sums an example any form of the kernels makes, for the workspace: blocks * chunks, with at most H blocks
 inline long qk_most_sums(int B, int T, int H) {
     if (H <= 0) return 0;
-    const long chunks = clamp_int(4L * kNumSMs / B, 1, T / 16 > 0 ? T / 16 : 1);
-    return chunks * H < 4L * kNumSMs / B + H ? chunks * H : 4L * kNumSMs / B + H;
+    const long by_waves = 4 * kQkResident / B + H, by_length = (long)H * (T / 16 > 0 ? T / 16 : 1);
+    return by_waves < by_length ? by_waves : by_length;
 }
 
 int qk_check(const dpclip_heads* parts, int n_parts, int B, int T, int D, int rot_dim, const float* table, long n_pos,
@@ -600,7 +612,7 @@ int dpclip_qknorm_backward(const dpclip_heads* parts, int n_parts, int B, int T,
     }
     const bool ring = qk_ring_backward(s, B, T, p.part);
     for (int k = 0; k < n_parts; ++k) {
-        p.part[k].chunks = qk_chunks(B, T, p.part[0].blocks + p.part[1].blocks, ring);
+        p.part[k].chunks = qk_chunks(B, T, p.part[0].blocks + p.part[1].blocks);
         sums[k] = (size_t)p.part[k].blocks * p.part[k].chunks;
     }
     if (!workspace || !is_aligned(workspace, 16) || workspace_bytes < kHeaderBytes + sizeof(float) * B * (sums[0] + sums[1]) * D)
