@@ -481,16 +481,55 @@ constexpr int BK = 64, BM_CTA = 128;
 constexpr int A_BYTES = BM_CTA * 128;                    // 128 rows x 64 bf16
 constexpr int BOX_BYTES = 32 * 128;                      // 32 rows x 64 bf16 of an output
 // Epilogue warps and the boxes of outputs they stage.  Forward: 16 warps, each 32 rows x 32 columns of h (and of zg, zu); two neighbours fill a
-// box together.  (With 8 warps of 64 columns the epilogue's latency, not its 0.24 of the issue slots, paced the kernel: 133 us.)  Backward: 8
-// warps, each 32 rows x HN columns of dx.
+// box together.  (With 8 warps of 64 columns the epilogue's latency, not its 0.24 of the issue slots, paced the kernel: 133 us.)  h is staged where
+// zg was, once that has left: a box less leaves shared memory for another stage (32768 x 512 -> 2048 with z: 137 -> 132 us).  Backward: 8 warps,
+// each 32 rows x HN columns of dx.
 template <bool FWD, bool KEEP, int HN> struct Cfg {
     static constexpr int EPI_WARPS = FWD ? 16 : 8, THREADS = 64 + 32 * EPI_WARPS;
-    static constexpr int BOXES = FWD ? (KEEP ? 3 : 1) : HN / 64;         // of a pair of warps, or of a warp
+    static constexpr int BOXES = FWD ? (KEEP ? 2 : 1) : HN / 64;         // of a pair of warps, or of a warp
     static constexpr int STAGE_BYTES = A_BYTES + HN * 128;
     static constexpr int STAGING = 8 * BOXES * BOX_BYTES;
     static constexpr int STAGES = (224 * 1024 - STAGING) / STAGE_BYTES;
     static constexpr int SMEM_BYTES = STAGES * STAGE_BYTES + STAGING + 256 + 1024;
 };
+// Rows r0 .. r1 - 1 (r0 a multiple of 8) of a box to rows that TMA cannot address (bases or lengths that are no multiple of 16 bytes): a row's
+// 64 columns per warp, as 32-bit words from its first 4-byte boundary on.  The path is bound by instructions, so what depends on a row's
+// parity alone (odd lengths alternate) is worked out once for the even and once for the odd rows (20000 x 576 -> 1170 with z kept: 103 us; element
+// by element 124; the same with 1176 columns by TMA 69).  `n`: columns there are.
+__device__ __forceinline__ void box_rows_out(const uint8_t* box, __nv_bfloat16* to, long ld, int r0, int r1, int n, int lane) {
+    uint32_t lo[2], hi[2];
+    __nv_bfloat16* at[2];
+    bool word[2], single[2], first[2];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        __nv_bfloat16* const row = to + (r0 + k) * ld;
+        const int odd = (int)(reinterpret_cast<uintptr_t>(row) >> 1) & 1, e = 2 * lane + odd;
+        at[k] = row + e;
+        word[k] = e + 1 < min(n, 64);
+        single[k] = e < n && !word[k];
+        first[k] = odd && lane == 31;                            // its second element is the row's first
+        lo[k] = e * 2; hi[k] = ((e + 1) & 63) * 2;
+    }
+    const uint32_t src = smem_u32(box);
+#pragma unroll 1
+    for (int r = r0; r < r1; r += 8) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int k = j & 1;
+            uint16_t x, y;
+            asm volatile("ld.shared.u16 %0, [%1];" : "=h"(x) : "r"(src + r * 128 + j * 128 + (lo[k] ^ (j << 4))));
+            asm volatile("ld.shared.u16 %0, [%1];" : "=h"(y) : "r"(src + r * 128 + j * 128 + (hi[k] ^ (j << 4))));
+            __nv_bfloat16* const q = at[k] + (j >> 1) * 2 * ld;
+            if (r + j < r1) {
+                if (word[k]) *reinterpret_cast<uint32_t*>(q) = (uint32_t)x | (uint32_t)y << 16;
+                if (single[k]) *reinterpret_cast<uint16_t*>(q) = x;
+                if (first[k]) *reinterpret_cast<uint16_t*>(q - 63) = y;
+            }
+        }
+        at[0] += 8 * ld;
+        at[1] += 8 * ld;
+    }
+}
 struct Maps { CUtensorMap a, b[2], h, z[2]; };           // b: rows of CTA 0 and of CTA 1; h: output (dx); z: gate and up halves of Z
 struct Params {
     int KB;                              // stages of the contraction
@@ -663,10 +702,11 @@ gated_tc_kernel(const __grid_constant__ gt::Maps maps, const __grid_constant__ g
                 }
                 continue;
             }
+            auto step = [&] { asm volatile("bar.sync %0, 64;" ::"r"(pair_bar) : "memory"); };     // the two warps of a box
             if (stores) bulk_wait_read();                                    // the box's last tile has left
-            asm volatile("bar.sync %0, 64;" ::"r"(pair_bar) : "memory");
+            step();
             if (!ok) {
-                asm volatile("bar.sync %0, 64;" ::"r"(pair_bar) : "memory");
+                for (int i = 0; i < (KEEP ? 3 : 1); ++i) step();
                 continue;
             }
             // 32 columns of a row = four 16-byte slots of a 128-byte row, at their swizzled places
@@ -690,7 +730,26 @@ gated_tc_kernel(const __grid_constant__ gt::Maps maps, const __grid_constant__ g
                         u[j] = __float_as_uint(__uint_as_float(u[j]) + __ldg(o.bias + o.F + col + j));
                     }
             }
-            if (KEEP) { put(mine + BOX_BYTES, g); put(mine + 2 * BOX_BYTES, u); }
+            // the box to h, or both to the halves of z
+            auto send = [&](bool is_z) {
+                if (p.tma_out) fence_proxy_async_smem();
+                step();
+                if (p.tma_out) {
+                    if (stores) {
+                        if (is_z) { tma_store_2d(&maps.z[0], boxes, box_col, row0); tma_store_2d(&maps.z[1], boxes + BOX_BYTES, box_col, row0); }
+                        else tma_store_2d(&maps.h, boxes, box_col, row0);
+                        bulk_commit();
+                    }
+                    return;
+                }
+                const int r0 = (group & 1) * 16, r1 = min(r0 + 16, o.M - row0);
+                __nv_bfloat16* const to = static_cast<__nv_bfloat16*>(is_z ? o.z : o.h);
+                const long ld = is_z ? o.ldz : o.ldh;
+#pragma unroll 1
+                for (int b = 0; b < (is_z ? 2 : 1); ++b)
+                    box_rows_out(boxes + b * BOX_BYTES, to + (long)row0 * ld + (b ? o.F : 0) + box_col, ld, r0, r1, o.F - box_col, lane);
+            };
+            if (KEEP) { put(mine, g); put(mine + BOX_BYTES, u); send(true); }
             gate_dispatch<false>(o.act, [&](auto a) {
 #pragma unroll
                 for (int j = 0; j < 32; j += 2) {
@@ -701,29 +760,12 @@ gated_tc_kernel(const __grid_constant__ gt::Maps maps, const __grid_constant__ g
                     g[j] = __float_as_uint(x); g[j + 1] = __float_as_uint(y);
                 }
             });
-            put(mine, g);
-            if (p.tma_out) fence_proxy_async_smem();
-            asm volatile("bar.sync %0, 64;" ::"r"(pair_bar) : "memory");
-            if (p.tma_out) {
-                if (stores) {
-                    tma_store_2d(&maps.h, boxes, box_col, row0);
-                    if (KEEP) { tma_store_2d(&maps.z[0], boxes + BOX_BYTES, box_col, row0); tma_store_2d(&maps.z[1], boxes + 2 * BOX_BYTES, box_col, row0); }
-                    bulk_commit();
-                }
-            } else {
-                // rows that TMA cannot address: element by element, the lanes along a row; each warp its own 32 columns
-#pragma unroll 1
-                for (int b = 0; b < C::BOXES; ++b) {
-                    __nv_bfloat16* const base = static_cast<__nv_bfloat16*>(b > 0 ? o.z : o.h) + (b == 2 ? o.F : 0);
-                    const long ld = b > 0 ? o.ldz : o.ldh;
-                    const int e = (group & 1) * 32 + lane;
-#pragma unroll 4
-                    for (int r = 0; r < 32; ++r) {
-                        const __nv_bfloat16 v = *reinterpret_cast<const __nv_bfloat16*>(boxes + b * BOX_BYTES + r * 128 + (((e >> 3) ^ (r & 7)) << 4) + (e & 7) * 2);
-                        if (row0 + r < o.M && col + lane < o.F) base[(long)(row0 + r) * ld + col + lane] = v;
-                    }
-                }
+            if (KEEP) {                                                      // h goes where zg was
+                if (stores) bulk_wait_read();
+                step();
             }
+            put(mine, g);
+            send(false);
         }
         if (stores) bulk_wait();
     } else {
@@ -784,16 +826,12 @@ gated_tc_kernel(const __grid_constant__ gt::Maps maps, const __grid_constant__ g
                     bulk_commit();
                 }
             } else {
+                __syncwarp();
 #pragma unroll 1
                 for (int b = 0; b < C::BOXES; ++b) {
-                    __nv_bfloat16* const base = static_cast<__nv_bfloat16*>(o.h);
                     const int cb = col0 + b * 64;
-#pragma unroll 4
-                    for (int i = 0; i < 64; ++i) {
-                        const int r = i >> 1, e = (i & 1) * 32 + lane;
-                        const __nv_bfloat16 v = *reinterpret_cast<const __nv_bfloat16*>(boxes + b * BOX_BYTES + r * 128 + (((e >> 3) ^ (r & 7)) << 4) + (e & 7) * 2);
-                        if (row0 + r < o.M && cb + e < o.F) base[(long)(row0 + r) * o.ldh + cb + e] = v;
-                    }
+                    if (cb < o.F)
+                        box_rows_out(boxes + b * BOX_BYTES, static_cast<__nv_bfloat16*>(o.h) + (long)row0 * o.ldh + cb, o.ldh, 0, min(32, o.M - row0), o.F - cb, lane);
                 }
                 __syncwarp();
             }
