@@ -725,8 +725,11 @@ int dpclip_gated_backward(const void* dH, long lddh, const void* Z, long ldz, co
     const long v = dtype == DPCLIP_F32 ? 4 : 8;
     const bool vec = is_aligned(dH, 16) && is_aligned(Z, 16) && is_aligned(dZ, 16) && F % v == 0 && lddh % v == 0 && ldz % v == 0 && lddz % v == 0;
     s.per_row = vec ? F / (int)v : F;
-    const int tall = s.per_row < 256 ? 256 / s.per_row : 1;
-    const int grid = clamp_int(((long)M + tall - 1) / tall, 1, kNumSMs * 8);
+    const int along = vec ? s.per_row : ceil_div(s.per_row, 4);
+    s.wide = along < 256 ? along : 256;
+    const long rows = ceil_div(M, 256 / s.wide);
+    const int grid_x = clamp_int(rows, 1, kNumSMs * 8);
+    const dim3 grid(grid_x, clamp_int(kNumSMs * 2 / grid_x, 1, ceil_div(along, s.wide)));
     if (dtype == DPCLIP_F32) {
         if (vec) gated_signal_kernel<float, 4><<<grid, 256, 0, st>>>(s);
         else gated_signal_kernel<float, 1><<<grid, 256, 0, st>>>(s);

@@ -19,9 +19,14 @@
 namespace dpclip {
 
 // ------------------------------------------------------------------------------------------------ activations
-// EXACT: expf and a correctly rounded division, for fp32 results; else the fast forms (a few 2^-21), for bf16 ones.
+// EXACT: expf and one step of Newton's iteration r + r (1 - d r) on the hardware's reciprocal (2^-22 before it), for fp32 results; else the
+// fast forms (a few 2^-21), for bf16 ones.  Division proper branches for every element: 1.8 us a tile of 256 x 128 in the fp32 epilogue.  Where d is
+// above 2^126 the sigmoid is zero (it is below 1.2e-38, and an infinite d would make the step NaN).
+__device__ __forceinline__ float gate_rcp(float x) { float r; asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x)); return r; }
 template <bool EXACT> __device__ __forceinline__ float gate_sigmoid(float z) {
-    return EXACT ? 1.f / (1.f + expf(-z)) : __fdividef(1.f, 1.f + __expf(-z));
+    if constexpr (!EXACT) return __fdividef(1.f, 1.f + __expf(-z));
+    const float d = 1.f + expf(-z), r = gate_rcp(d);
+    return d > 8.5070592e37f ? 0.f : fmaf(r, fmaf(-d, r, 1.f), r);
 }
 constexpr float kGeluTanh = 0.7978845608028654f, kGeluCube = 0.044715f;       // sqrt(2 / pi)
 
@@ -55,7 +60,6 @@ template <int ACT, bool EXACT> __device__ __forceinline__ void gate_act_grad(flo
 // epilogue of the tensor-core kernel is made of little else (per element two of them and three multiply-adds; one element at a time, with
 // __expf and __fdividef, it was 21 instructions and bound the kernel).
 __device__ __forceinline__ float gate_ex2(float x) { float r; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x)); return r; }
-__device__ __forceinline__ float gate_rcp(float x) { float r; asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x)); return r; }
 constexpr float kLog2e = 1.4426950408889634f;
 template <int ACT> __device__ __forceinline__ f32x2 gate_pair(f32x2 g, f32x2 u) {
     if constexpr (ACT == DPCLIP_ACT_SILU || ACT == DPCLIP_ACT_GELU_TANH) {
@@ -136,7 +140,7 @@ struct GatedSignal {
     void* dz; long lddz;                 // [M][2F], may be z
     __nv_bfloat16* copy; long ldc;       // NULL, or rows of 16-byte multiples for the product: bf16 a copy of dz, fp32 its three planes
     long plane;
-    long M; int F, act, per_row;         // per_row: groups of V elements a row of h
+    long M; int F, act, per_row, wide;   // per_row: groups of V elements a row of h; wide: threads a row
 };
 template <typename T> __device__ __forceinline__ void gated_copy_out(const GatedSignal& p, long m, int f, float v) {
     __nv_bfloat16* const to = p.copy + m * p.ldc + f;
@@ -148,13 +152,13 @@ template <typename T> __device__ __forceinline__ void gated_copy_out(const Gated
         for (int j = 0; j < 3; ++j) *reinterpret_cast<uint16_t*>(to + j * p.plane) = t[j];
     }
 }
-// 256 threads: as many rows side by side as fit, a row's groups along the threads.
+// 256 threads: as many rows side by side as fit, a row's groups along the threads; with few rows a row's groups go to gridDim.y CTAs.
 template <typename T, int V>             // V elements a thread: 16 bytes, or one
 __global__ void __launch_bounds__(256)
 gated_signal_kernel(const __grid_constant__ GatedSignal p) {
     constexpr bool EXACT = sizeof(T) == 4;
     griddep_launch_dependents();
-    const int wide = min(p.per_row, 256), tall = 256 / wide, ty = threadIdx.x / wide, tx = threadIdx.x - ty * wide;
+    const int wide = p.wide, tall = 256 / wide, ty = threadIdx.x / wide, tx = threadIdx.x - ty * wide + blockIdx.y * wide, step = gridDim.y * wide;
     if (ty >= tall) return;
     gate_dispatch<EXACT>(p.act, [&](auto a) {
         constexpr int ACT = decltype(a)::value;
@@ -169,16 +173,31 @@ gated_signal_kernel(const __grid_constant__ GatedSignal p) {
                 du = h * act;
             };
             if constexpr (V == 1) {
-#pragma unroll 4
-                for (int f = tx; f < p.per_row; f += wide) {
-                    float dg, du;
-                    one(to_f32(dh[f]), to_f32(zg[f]), to_f32(zg[p.F + f]), dg, du);
-                    gate_store(og + f, dg); gate_store(og + p.F + f, du);
-                    if (p.copy) { gated_copy_out<T>(p, m, f, dg); gated_copy_out<T>(p, m, p.F + f, du); }
+                // four elements a thread in flight
+                for (int f0 = tx; f0 < p.per_row; f0 += 4 * step) {
+                    float h[4], g[4], u[4], dg[4], du[4];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const int f = f0 + j * step;
+                        const bool there = f < p.per_row;
+                        h[j] = there ? to_f32(dh[f]) : 0.f;
+                        g[j] = there ? to_f32(zg[f]) : 0.f;
+                        u[j] = there ? to_f32(zg[p.F + f]) : 0.f;
+                    }
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) one(h[j], g[j], u[j], dg[j], du[j]);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const int f = f0 + j * step;
+                        if (f < p.per_row) {
+                            gate_store(og + f, dg[j]); gate_store(og + p.F + f, du[j]);
+                            if (p.copy) { gated_copy_out<T>(p, m, f, dg[j]); gated_copy_out<T>(p, m, p.F + f, du[j]); }
+                        }
+                    }
                 }
             } else {
 #pragma unroll 2
-                for (int c = tx; c < p.per_row; c += wide) {
+                for (int c = tx; c < p.per_row; c += step) {
                     const int f = c * V;
                     const uint4 h = *reinterpret_cast<const uint4*>(dh + f), g = *reinterpret_cast<const uint4*>(zg + f),
                                 u = *reinterpret_cast<const uint4*>(zg + p.F + f);

@@ -10,7 +10,7 @@
 // correctly rounded, while the next window is multiplied in the other accumulator.
 //
 // Bound: the six products, about 1.4 PFLOP/s / 6; 3850 x 300 x 1100 with stored pre-activations: the splits and 51 MB of outputs weigh as
-// much.  The fp32 ALUs (gated_simt_kernel) reach 32 TFLOP/s on the same call.
+// much (45 us).  The fp32 ALUs (gated_simt_kernel) reach 32 TFLOP/s on the same call.
 #pragma once
 #include "kernels_gated.cuh"
 
@@ -185,6 +185,10 @@ gated_tc3_kernel(const __grid_constant__ gt3::Maps maps, const __grid_constant__
             int tm, tn, kb0, kb1;
             const int split = tile_at(t, tm, tn, kb0, kb1);
             const int row0 = tm * 2 * BM_CTA + (int)rank * BM_CTA + quarter * 32;
+            const int col0 = tn * (FWD ? HN : N) + at0, col1 = FWD ? col0 : col0 + CW;
+            // A lane's share of the biases, for shuffles in the epilogue; loads there, one a column and lane, were 1.5 us a tile.
+            float bias_g = 0.f, bias_u = 0.f;
+            if (FWD && o.bias && lane < CW && col0 + lane < o.F) { bias_g = __ldg(o.bias + col0 + lane); bias_u = __ldg(o.bias + o.F + col0 + lane); }
             float x[2][CW];
 #pragma unroll
             for (int j = 0; j < CW; ++j) { x[0][j] = 0.f; x[1][j] = 0.f; }
@@ -208,7 +212,6 @@ gated_tc3_kernel(const __grid_constant__ gt3::Maps maps, const __grid_constant__
                 if (lane == 0) mbar_arrive_cluster(acc_empty0 + buf * 8);
             }
             if (!ok) break;
-            const int col0 = tn * (FWD ? HN : N) + at0, col1 = FWD ? col0 : col0 + CW;
             if (row0 >= o.M || col0 >= o.F) continue;
             // 16 columns of 32 rows, from a row a lane to 64-byte runs
             auto put = [&](const float* v, float* base, long ld, int col, bool vec) {
@@ -248,8 +251,7 @@ gated_tc3_kernel(const __grid_constant__ gt3::Maps maps, const __grid_constant__
             if constexpr (FWD) {
                 if (o.bias) {
 #pragma unroll
-                    for (int j = 0; j < CW; ++j)
-                        if (col0 + j < o.F) { x[0][j] += __ldg(o.bias + col0 + j); x[1][j] += __ldg(o.bias + o.F + col0 + j); }
+                    for (int j = 0; j < CW; ++j) { x[0][j] += __shfl_sync(0xFFFFFFFFu, bias_g, j); x[1][j] += __shfl_sync(0xFFFFFFFFu, bias_u, j); }
                 }
                 if (o.z) {
                     float* const z = static_cast<float*>(o.z);

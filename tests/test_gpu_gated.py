@@ -373,3 +373,39 @@ def test_two_streams_at_once(dp, dtype):
     torch.cuda.synchronize()
     for s, w in zip(sides, want):
         assert all(torch.equal(a, b) for a, b in zip(s[2], w)) and dp.dpclip_read_status(s[3]) == 0
+
+
+@pytest.mark.parametrize("shape", [(1, 24, 4003), (3, 40, 5008), (5, 16, 1031), (40, 24, 2049)])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("layout", ["dense", "odd"])
+def test_backward_few_long_rows(dp, dtype, shape, layout):
+    test_backward(dp, dtype, shape, layout, "gelu_tanh")
+
+
+@pytest.mark.parametrize("layout", ["dense", "odd"])
+def test_fp32_silu_over_its_range(dp, layout):
+    """silu and its slope from z alone (dh = u = 1), against 64 bits.
+
+    In units of 2^-24: the exponential is off by 4, the addition of 1 and Newton's step by 1 each and the square of the reciprocal's 2^-22 is
+    nothing, so p = sigmoid(z) is off by 6 p, z p by 7 |z| p.  The slope p (1 + z (1 - p)): 1 - p is off by 1 + 6 p, so the bracket by
+    |z| (1 + 6 p) + 1 + |z|, the product by 7 (1 + |z|) p more: at most 16 (1 + |z|) p together.  Below 2^-126 p is zero: z p is then off by
+    88 x 2^-126.
+    """
+    z = torch.cat([torch.linspace(-120, 120, 60001), torch.linspace(-2, 2, 4000), torch.tensor([0.0, -0.0, 1e-30, -1e-30, 1e30])]).float()
+    M, F = 1, z.numel()
+    Z = rows(torch.stack([z, torch.ones_like(z)]).reshape(1, 2 * F), layout, F32)
+    dH, dZ = rows(torch.ones((M, F)), layout, F32), rows(torch.zeros((M, 2 * F)), layout, F32)
+    dp.dpclip_gated_backward(dH, Z, None, dZ, None, dp.DPCLIP_ACT_SILU, workspace(dp, dp.dpclip_gated_workspace_bytes(M, 8, F, CODE[F32])))
+    got = dZ.cpu().double().reshape(2, F)
+    z = z.double()
+    p = 1 / (1 + torch.exp(-z))
+    tiny = 88 * 2.0 ** -126
+    assert ((got[1] - z * p).abs() <= 7 * U32 * z.abs() * p + tiny).all()
+    slope = p * (1 + z * (1 - p))
+    assert ((got[0] - slope).abs() <= 16 * U32 * (1 + z.abs()) * p + tiny).all()
+    # a NaN stays one, an infinity gives what the formula gives
+    ends = rows(torch.tensor([[float("nan"), float("inf"), -float("inf"), 1.0, 1.0, 1.0]]), layout, F32)
+    dZ = rows(torch.zeros((1, 6)), layout, F32)
+    dp.dpclip_gated_backward(rows(torch.ones((1, 3)), layout, F32), ends, None, dZ, None, dp.DPCLIP_ACT_SILU, workspace(dp, dp.dpclip_gated_workspace_bytes(1, 8, 3, CODE[F32])))
+    value = dZ.cpu()[0, 3:]
+    assert value[0].isnan() and value[1] == float("inf") and value[2].isnan()
