@@ -282,7 +282,7 @@ GatedCut gated_cut(long M, long cols, long KD, bool fwd, bool f32) {
     GatedCut best = {128, 1, KB};
     double least = 1e30;
     for (int hn = 64; hn <= 128; hn *= 2)
-        for (int s = 1; s <= 32; s *= 2) {
+        for (int s = 1; s <= 32; ++s) {
             if (s > 1 && KB < (f32 ? 2 : 4) * s) break;
             const long tiles = (long)ceil_div(M, 256) * ceil_div(cols, fwd ? hn : 2 * hn);
             if (s > 1 && tiles * s > 2 * kPairs) break;

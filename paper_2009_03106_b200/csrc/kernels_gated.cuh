@@ -695,6 +695,8 @@ gated_tc_kernel(const __grid_constant__ gt::Maps maps, const __grid_constant__ g
             const int buf = it & 1;
             const int row0 = w.m * 2 * BM_CTA + (int)rank * BM_CTA + quarter * 32;
             const int box_col = w.n * HN + box * 64, col = box_col + (group & 1) * 32;
+            float bias_g = 0.f, bias_u = 0.f;                                // of column `lane`: to the others by shuffle
+            if (o.bias && col + lane < o.F && o.splits == 1) { bias_g = __ldg(o.bias + col + lane); bias_u = __ldg(o.bias + o.F + col + lane); }
             // A wait that ran out must not leave the box's other warp at a barrier: from then on both only keep step.
             ok = __all_sync(0xFFFFFFFFu, ok && mbar_wait(&acc_full[buf], (it >> 1) & 1, abort_flag, p.status));
             tc_fence_after_sync();
@@ -743,11 +745,10 @@ gated_tc_kernel(const __grid_constant__ gt::Maps maps, const __grid_constant__ g
             };
             if (o.bias) {
 #pragma unroll
-                for (int j = 0; j < 32; ++j)
-                    if (col + j < o.F) {
-                        g[j] = __float_as_uint(__uint_as_float(g[j]) + __ldg(o.bias + col + j));
-                        u[j] = __float_as_uint(__uint_as_float(u[j]) + __ldg(o.bias + o.F + col + j));
-                    }
+                for (int j = 0; j < 32; ++j) {
+                    g[j] = __float_as_uint(__uint_as_float(g[j]) + __shfl_sync(0xFFFFFFFFu, bias_g, j));
+                    u[j] = __float_as_uint(__uint_as_float(u[j]) + __shfl_sync(0xFFFFFFFFu, bias_u, j));
+                }
             }
             // the box to h, or both to the halves of z
             auto send = [&](bool is_z) {
