@@ -82,7 +82,11 @@ struct Args {
         if (x == -1.0 && PyErr_Occurred()) { PyErr_Clear(); throw BadType("expected a number"); }
         return x;
     }
-    bool truth(int i) const { return PyObject_IsTrue(v[i]) == 1; }
+    bool truth(int i) const {
+        const int x = PyObject_IsTrue(v[i]);
+        if (x < 0) { PyErr_Clear(); throw BadType("expected a truth value"); }
+        return x == 1;
+    }
 };
 
 // Tensors lie on the current device, where the calls run.
@@ -118,6 +122,11 @@ float* dense_f32(const at::Tensor* t, at::IntArrayRef sizes, const char* what) {
 void writable(const at::Tensor& t, const char* what) {
     for (int64_t i = 0; i < t.dim(); ++i)
         if (t.stride(i) == 0 && t.size(i) > 1) throw BadValue(std::string(what) + ": an output may not be a broadcast tensor");
+}
+// a workspace owns every byte that it counts: an expanded tensor would not
+const at::Tensor& workspace_of(const at::Tensor& t) {
+    if (!t.is_contiguous()) throw BadValue("workspace: expected a contiguous tensor");
+    return t;
 }
 int size32(int64_t n) {
     if (n > INT_MAX) throw BadValue("a dimension is out of range");
@@ -179,7 +188,7 @@ PyObject* relbias_forward(PyObject*, PyObject* const* v, Py_ssize_t n) {
 PyObject* relbias_sqnorms(PyObject*, PyObject* const* v, Py_ssize_t n) {
     return guarded([&] {
         const Args a(v, n, 12);
-        const at::Tensor& dS = a.tensor(0), &grads = a.tensor(1), &sq = a.tensor(2), &ws = a.tensor(3);
+        const at::Tensor& dS = a.tensor(0), &grads = a.tensor(1), &sq = a.tensor(2), &ws = workspace_of(a.tensor(3));
         const at::Tensor* ql = a.maybe(8), *kl = a.maybe(9);
         Device d;
         d.check(&dS); d.check(&grads); d.check(&sq); d.check(&ws); d.check(ql); d.check(kl);
@@ -252,7 +261,7 @@ PyObject* qknorm_forward(PyObject*, PyObject* const* v, Py_ssize_t n) {
 PyObject* qknorm_backward(PyObject*, PyObject* const* v, Py_ssize_t n) {
     return guarded([&] {
         const Args a(v, n, 20);
-        const at::Tensor& q = a.tensor(2), &ws = a.tensor(13);
+        const at::Tensor& q = a.tensor(2), &ws = workspace_of(a.tensor(13));
         const at::Tensor* k = a.maybe(3);
         Device d;
         if (q.dim() != 4) throw BadValue("q must be (B, T, H, D)");
@@ -301,7 +310,7 @@ Matrix matrix_of(Device& d, const at::Tensor& t, at::ScalarType type, int64_t ro
 PyObject* gated_forward(PyObject*, PyObject* const* v, Py_ssize_t n) {
     return guarded([&] {
         const Args a(v, n, 8);
-        const at::Tensor& X = a.tensor(0), &Wt = a.tensor(1), &Ht = a.tensor(3), &ws = a.tensor(6);
+        const at::Tensor& X = a.tensor(0), &Wt = a.tensor(1), &Ht = a.tensor(3), &ws = workspace_of(a.tensor(6));
         const at::Tensor* bias = a.maybe(2), *Zt = a.maybe(4);
         Device d;
         const auto type = X.scalar_type();
@@ -339,6 +348,7 @@ PyObject* gated_backward(PyObject*, PyObject* const* v, Py_ssize_t n) {
             writable(*dXt, "dX");
         }
         d.check(ws);
+        if (ws) workspace_of(*ws);
         return lib.dpclip_gated_backward(dh.p, dh.ld, z.p, z.ld, w.p, w.ld, size32(z.rows), size32(w.cols), size32(F), dtype_of(Zt), (dpclip_activation)a.int32(5),
                                          dz.p, dz.ld, dx.p, dx.ld, ws ? ws->data_ptr() : nullptr, ws ? ws->nbytes() : 0, stream_of(v[7]));
     });

@@ -193,3 +193,18 @@ def test_host_tensors_are_refused(dp):
         dp.dpclip_relbias_forward(torch.zeros(32, 4), torch.zeros(4, 2, 2), 128)
     with pytest.raises(ValueError):
         dp.dpclip_stored_clipped_grad(torch.zeros(2, 4), None, torch.zeros(4))
+
+
+def test_expanded_workspaces_are_refused(dp):
+    """An expanded tensor counts bytes that it does not own; the refusal comes before anything about devices."""
+    import torch
+    ws = torch.zeros((1,), dtype=torch.uint8).expand(1 << 24)
+    t = lambda *s: torch.zeros(s)                                             # noqa: E731
+    calls = [
+        lambda: dp.dpclip_relbias_sqnorms(t(1, 1, 4, 4), t(1, 8, 1), t(1), ws, 64),
+        lambda: dp.dpclip_qknorm_backward(t(1, 4, 1, 8), None, t(1, 4, 1, 8), None, t(8), None, None, t(1, 4, 1, 8), None, t(1, 8), None, t(1), None, ws),
+        lambda: dp.dpclip_gated_forward(t(4, 8), t(16, 8), None, t(4, 8), None, dp.DPCLIP_ACT_SILU, ws),
+    ]
+    for call in calls:
+        with pytest.raises(ValueError, match="workspace"):
+            call()

@@ -409,3 +409,13 @@ def test_fp32_silu_over_its_range(dp, layout):
     dp.dpclip_gated_backward(rows(torch.ones((1, 3)), layout, F32), ends, None, dZ, None, dp.DPCLIP_ACT_SILU, workspace(dp, dp.dpclip_gated_workspace_bytes(1, 8, 3, CODE[F32])))
     value = dZ.cpu()[0, 3:]
     assert value[0].isnan() and value[1] == float("inf") and value[2].isnan()
+
+
+def test_expanded_workspace_and_flags_without_a_truth_value_are_refused(dp):
+    """By the host, before a launch."""
+    t = lambda *s: torch.zeros(s, device="cuda")                              # noqa: E731
+    ws = torch.zeros((1,), dtype=torch.uint8, device="cuda").expand(1 << 24)
+    with pytest.raises(ValueError, match="workspace"):
+        dp.dpclip_gated_backward(t(4, 8), t(4, 16), t(16, 8), t(4, 16), t(4, 8), dp.DPCLIP_ACT_SILU, ws)
+    with pytest.raises(TypeError, match="truth"):
+        dp.dpclip_relbias_forward(t(8, 1), t(1, 4, 4), 64, bidirectional=torch.zeros(2))
