@@ -12,7 +12,7 @@
 //
 // Bound: memory in long calls (every input is read once, every output written once), round trips in short ones.  The backward pass computes
 // rms(x) again from the x it reads anyway, so the forward pass stores nothing for it.  128 x 256 tokens in bf16: 8 + 8 heads of 64 in 30 us (134
-// MB, what a copy takes), backward 16 + 2 heads of 128 in 113 us (453 MB).
+// MB, what a copy takes), backward 16 + 2 heads of 128 in 105 us (453 MB).
 #pragma once
 #include "common.cuh"
 
@@ -366,7 +366,7 @@ qknorm_backward_kernel(const __grid_constant__ QkParams p) {
 // The same passes with the loads taken out of the way: every lane copies its own runs of the warp's next tokens into shared memory
 // (cp.async, 16 bytes, zero-filled where nothing is read), STAGES - 1 of them ahead, and reads back only what it copied itself, so a warp
 // waits for its own copies and for no other warp.  With loads to registers, four heads in flight a group, the forward pass took 38 us where it
-// takes 30, the backward pass 135 (113).  A warp stays with one block of heads.
+// takes 30, the backward pass 135 (113; 105 since its chunks fill whole waves).  A warp stays with one block of heads.
 __device__ __forceinline__ void qk_copy16(uint32_t dst, const void* src, bool on) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(on ? 16 : 0) : "memory");
 }
