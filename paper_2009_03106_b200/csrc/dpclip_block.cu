@@ -288,7 +288,7 @@ GatedCut gated_cut(long M, long cols, long KD, bool fwd, bool f32) {
             if (s > 1 && tiles * s > 2 * kPairs) break;
             const int per = ceil_div(KB, s);
             double cost = (double)((tiles * s + kPairs - 1) / kPairs) * (per * (hn == 128 ? 1.0 : 0.6) * (f32 ? 6 : 1) + (f32 ? 12 : 6));
-            if (s > 1) cost += 10 + (double)M * cols * (fwd ? 2 : 1) * 4 * (s + 1) / 5e6 / 0.28;
+            if (s > 1) cost += 4 + (double)M * cols * (fwd ? 2 : 1) * 4 * (s + 1) / 5e6 / 0.28;
             if (cost < least) { least = cost; best = {hn, ceil_div(KB, per), per}; }
         }
     return best;

@@ -549,6 +549,31 @@ __device__ __forceinline__ void box_rows_out(const uint8_t* box, __nv_bfloat16* 
         at[1] += 8 * ld;
     }
 }
+// 16 fp32 columns from `col` on of a warp's 32 rows from row0 on, a row a lane, to 64-byte runs of a matrix of M rows and F columns: through 2 KB of the
+// warp's own (stored as they lie, 32 rows an instruction, the partial products made 304 x 4096 -> 1024 34 us where it takes 21).  vec: rows start at 16-byte boundaries.
+__device__ __forceinline__ void rows16_out(float4* mine, const float* v, float* base, long ld, int row0, int M, int col, int F, bool vec, int lane) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) mine[lane * 4 + (j ^ ((lane >> 1) & 3))] = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+    __syncwarp();
+    if (vec && col + 16 <= F) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int r = i * 8 + (lane >> 2), s = lane & 3;
+            if (row0 + r < M) *reinterpret_cast<float4*>(base + (long)(row0 + r) * ld + col + s * 4) = mine[r * 4 + (s ^ ((r >> 1) & 3))];
+        }
+    } else {
+        // rows at any address, or the last columns: one element a lane, sixteen lanes a row
+        const float* const flat = reinterpret_cast<const float*>(mine);
+        const int s = lane & 15, c = col + s;
+#pragma unroll 4
+        for (int i = 0; i < 16; ++i) {
+            const int r = i * 2 + (lane >> 4);
+            const float q = flat[r * 16 + (((s >> 2) ^ ((r >> 1) & 3)) << 2) + (s & 3)];
+            if (row0 + r < M && c < F) base[(long)(row0 + r) * ld + c] = q;
+        }
+    }
+    __syncwarp();
+}
 struct Maps { CUtensorMap a, b[2], h, z[2]; };           // b: rows of CTA 0 and of CTA 1; h: output (dx); z: gate and up halves of Z
 struct Params {
     int KB;                              // stages of the contraction
@@ -713,13 +738,16 @@ gated_tc_kernel(const __grid_constant__ gt::Maps maps, const __grid_constant__ g
             if (lane == 0 && ok) mbar_arrive_cluster(acc_empty0 + buf * 8);
             if (!there) continue;
             if (o.splits > 1) {
-                // partial products: a thread's row, 128 bytes of it
-                const int m = row0 + lane;
-                if (m < o.M && ok) {
-                    float* to = o.part + ((long)w.split * o.M + m) * 2L * o.F + col;
+                if (!ok) continue;
+                float* const part = o.part + (long)w.split * o.M * 2L * o.F;
+                float4* const mine = reinterpret_cast<float4*>(boxes + (group & 1) * 2048);
+                float v[32], x[32];
 #pragma unroll
-                    for (int j = 0; j < 32; ++j)
-                        if (col + j < o.F) { to[j] = __uint_as_float(g[j]); to[o.F + j] = __uint_as_float(u[j]); }
+                for (int j = 0; j < 32; ++j) { v[j] = __uint_as_float(g[j]); x[j] = __uint_as_float(u[j]); }
+#pragma unroll
+                for (int c = 0; c < 32; c += 16) {
+                    rows16_out(mine, v + c, part, 2L * o.F, row0, o.M, col + c, o.F, o.F % 4 == 0, lane);
+                    rows16_out(mine, x + c, part + o.F, 2L * o.F, row0, o.M, col + c, o.F, o.F % 4 == 0, lane);
                 }
                 continue;
             }
@@ -813,12 +841,12 @@ gated_tc_kernel(const __grid_constant__ gt::Maps maps, const __grid_constant__ g
                 tmem_ld_wait();
                 const int col = col0 + c * 32;
                 if (o.splits > 1) {
-                    const int m = row0 + lane;
-                    if (m < o.M) {
-                        float* to = o.part + ((long)w.split * o.M + m) * o.F + col;
+                    float v[32];
 #pragma unroll
-                        for (int j = 0; j < 32; ++j) if (col + j < o.F) to[j] = __uint_as_float(g[j]);
-                    }
+                    for (int j = 0; j < 32; ++j) v[j] = __uint_as_float(g[j]);
+#pragma unroll
+                    for (int j = 0; j < 32; j += 16)
+                        rows16_out(reinterpret_cast<float4*>(boxes), v + j, o.part + (long)w.split * o.M * o.F, o.F, row0, o.M, col + j, o.F, o.F % 4 == 0, lane);
                     continue;
                 }
                 uint8_t* const at = boxes + (c >> 1) * BOX_BYTES + lane * 128;

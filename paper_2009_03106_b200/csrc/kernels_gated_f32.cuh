@@ -213,30 +213,7 @@ gated_tc3_kernel(const __grid_constant__ gt3::Maps maps, const __grid_constant__
             }
             if (!ok) break;
             if (row0 >= o.M || col0 >= o.F) continue;
-            // 16 columns of 32 rows, from a row a lane to 64-byte runs
-            auto put = [&](const float* v, float* base, long ld, int col, bool vec) {
-#pragma unroll
-                for (int j = 0; j < 4; ++j) mine[lane * 4 + (j ^ ((lane >> 1) & 3))] = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
-                __syncwarp();
-                if (vec && col + 16 <= o.F) {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int r = i * 8 + (lane >> 2), s = lane & 3;
-                        if (row0 + r < o.M) *reinterpret_cast<float4*>(base + (long)(row0 + r) * ld + col + s * 4) = mine[r * 4 + (s ^ ((r >> 1) & 3))];
-                    }
-                } else {
-                    // rows at any address, or the last columns: one element a lane, sixteen lanes a row
-                    const float* const flat = reinterpret_cast<const float*>(mine);
-                    const int s = lane & 15, c = col + s;
-#pragma unroll 4
-                    for (int i = 0; i < 16; ++i) {
-                        const int r = i * 2 + (lane >> 4);
-                        const float q = flat[r * 16 + (((s >> 2) ^ ((r >> 1) & 3)) << 2) + (s & 3)];
-                        if (row0 + r < o.M && c < o.F) base[(long)(row0 + r) * ld + c] = q;
-                    }
-                }
-                __syncwarp();
-            };
+            auto put = [&](const float* v, float* base, long ld, int col, bool vec) { gt::rows16_out(mine, v, base, ld, row0, o.M, col, o.F, vec, lane); };
             if (o.splits > 1) {
                 const long width = FWD ? 2L * o.F : o.F;
                 float* const part = o.part + (long)split * o.M * width;

@@ -419,3 +419,12 @@ def test_expanded_workspace_and_flags_without_a_truth_value_are_refused(dp):
         dp.dpclip_gated_backward(t(4, 8), t(4, 16), t(16, 8), t(4, 16), t(4, 8), dp.DPCLIP_ACT_SILU, ws)
     with pytest.raises(TypeError, match="truth"):
         dp.dpclip_relbias_forward(t(8, 1), t(1, 4, 4), 64, bidirectional=torch.zeros(2))
+
+
+@pytest.mark.parametrize("shape", [(300, 1024, 161), (257, 2000, 30), (64, 1030, 1001), (513, 4097, 66)])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("layout", ["dense", "odd"])
+def test_split_contractions_with_ragged_ends(dp, dtype, shape, layout):
+    M, K, F = shape
+    test_forward(dp, dtype, shape, layout, "silu", True, True)
+    test_backward(dp, dtype, (M, F, K // 2), layout, "silu")
