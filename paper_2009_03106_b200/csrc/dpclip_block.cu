@@ -22,9 +22,30 @@ inline size_t round_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 inline int clamp_int(long v, long lo, long hi) { return (int)(v < lo ? lo : v > hi ? hi : v); }
 
 // ------------------------------------------------------------------------------------------------ relative position bias
+// A whole number of up to 128 factors of 25 bits.
+struct Whole {
+    uint32_t v[104];
+    int n;
+    Whole() : n(1) { v[0] = 1; }
+    void times(uint32_t f, int power) {
+        for (int i = 0; i < power; ++i) {
+            uint64_t carry = 0;
+            for (int j = 0; j < n; ++j) { carry += (uint64_t)v[j] * f; v[j] = (uint32_t)carry; carry >>= 32; }
+            if (carry) v[n++] = (uint32_t)carry;
+        }
+    }
+    bool below(const Whole& o) const {
+        if (n != o.n) return n < o.n;
+        for (int j = n - 1; j >= 0; --j)
+            if (v[j] != o.v[j]) return v[j] < o.v[j];
+        return false;
+    }
+};
+
 // thr[k], the smallest distance d of bucket exact + k: floor((n - exact) log(d / exact) / log(max / exact)) >= k, which is
-// d >= exact (max / exact)^(k / (n - exact)).  Borders that are whole numbers belong to the upper bucket; the powers are taken in extended
-// precision, where a border that is a whole number misses it by less than 1e-16 of itself.
+// d >= exact (max / exact)^(k / (n - exact)).  The borders are taken in extended precision, off by less than 1e-16 of themselves; one that
+// comes within 1e-15 of a whole number c is decided in whole numbers: c^m >= max^k exact^(m - k), m = n - exact.  A border can miss a whole
+// number by little without being one: 50 (2111336 / 50)^(43 / 50) is 475308.0000001.
 bool fill_buckets(RbBuckets& r, const dpclip_relbias* c) {
     if (!c || c->n_buckets < 2 || c->n_buckets > RB_MAX_BUCKETS) return false;
     if (c->bidirectional && c->n_buckets % 2) return false;
@@ -38,10 +59,17 @@ bool fill_buckets(RbBuckets& r, const dpclip_relbias* c) {
     if (r.exact < 1 || r.max_distance <= r.exact || r.max_distance > (1 << 24)) return false;
     const int m = r.n - r.exact;
     const long double step = powl((long double)r.max_distance / r.exact, 1.0L / m);
-    long double border = r.exact;                        // 128 steps at most: off by less than 1e-16 of itself at the last
+    long double border = r.exact;                        // 128 steps at most, each off by 2^-63
     for (int k = 0; k < m; ++k, border *= step) {
         const long double whole = roundl(border);
-        r.thr[k] = (int)(fabsl(border - whole) < 1e-12L * border ? whole : ceill(border));
+        r.thr[k] = (int)ceill(border);
+        if (k > 0 && fabsl(border - whole) < 1e-15L * border) {
+            Whole c, b;
+            c.times((uint32_t)whole, m);
+            b.times((uint32_t)r.max_distance, k);
+            b.times((uint32_t)r.exact, m - k);
+            r.thr[k] = (int)whole + (c.below(b) ? 1 : 0);
+        }
     }
     r.top = m > 1 ? 1 : 0;
     while (m > 1 && 2 * r.top < m) r.top *= 2;

@@ -54,6 +54,31 @@ def test_buckets_by_whole_numbers(dp, n_buckets, max_distance, bidirectional):
     assert dp.dpclip_relbias_bucket(-(1 << 40), n_buckets, max_distance, bidirectional) == (n_buckets // 2 if bidirectional else n_buckets) - 1
 
 
+def borders_of(n_buckets, max_distance):
+    """The smallest distance of every bucket on the logarithmic scale, one direction, by whole numbers."""
+    e = n_buckets // 2
+    m = n_buckets - e
+    for k in range(1, m):
+        lo, hi = e, max_distance
+        while lo < hi:
+            mid = (lo + hi) // 2
+            lo, hi = (lo, mid) if mid ** m * e ** k >= max_distance ** k * e ** m else (mid + 1, hi)
+        yield lo
+
+
+@pytest.mark.parametrize("n_buckets,max_distance", [
+    (100, 2111336), (200, 7419005), (100, 14515163),                # borders a millionth and less above a whole number
+    (16, 128), (32, 1024), (16, 1 << 19), (40, 20 << 19), (256, 1 << 24), (255, (1 << 24) - 3), (2, 2), (3, 2)])
+def test_both_sides_of_every_border(dp, n_buckets, max_distance):
+    for border in borders_of(n_buckets, max_distance):
+        for d in (border - 1, border):
+            want = bucket_of(-d, n_buckets, max_distance, False)
+            assert dp.dpclip_relbias_bucket(-d, n_buckets, max_distance, False) == want, d
+            if 2 * n_buckets <= 256:
+                assert dp.dpclip_relbias_bucket(-d, 2 * n_buckets, max_distance, True) == want, d
+                assert dp.dpclip_relbias_bucket(d, 2 * n_buckets, max_distance, True) == n_buckets + want, d
+
+
 @pytest.mark.parametrize("n_buckets,max_distance,bidirectional", [(1, 10, False), (0, 10, False), (257, 1000, False), (2, 10, True),
                                                                    (33, 100, True), (32, 8, True), (32, 16, False), (32, (1 << 24) + 1, False)])
 def test_bucket_settings_that_are_refused(dp, n_buckets, max_distance, bidirectional):
