@@ -323,7 +323,8 @@ qknorm_backward_kernel(const __grid_constant__ QkParams p) {
             qk_dot<V>(dots, qk_mul<V>(gb[n], gain1[n]), xb[n]);
         }
         const float sum = qk_group_sum<G>(sum_f32x2(ss)), dot = qk_group_sum<G>(sum_f32x2(dots));
-        const float r = now >= 0 ? rsqrtf(fmaf(sum, inv_d, p.eps)) : 0.f;
+        // a head that is not there counts as nothing: with eps = 0 the root of its zeros would be infinite
+        const float r = now >= 0 && head ? rsqrtf(fmaf(sum, inv_d, p.eps)) : 0.f;
         const QkVec<V> rr = qk_fill<V>(r), m = qk_fill<V>(-(dot * inv_d * r * r * r));   // m: what dx has of x
 #pragma unroll
         for (int n = 0; n < NCH; ++n) {
@@ -611,7 +612,8 @@ qknorm_backward_ring_kernel(const __grid_constant__ QkParams p) {
             qk_dot<V>(dots, qk_mul<V>(ga, qk_shared<V>(gain_a)), xa);
             qk_dot<V>(dots, qk_mul<V>(gb, qk_shared<V>(gain_b)), xb);
             const float sum = qk_group_sum<G>(sum_f32x2(ss)), dot = qk_group_sum<G>(sum_f32x2(dots));
-            const float r = at >= 0 ? rsqrtf(fmaf(sum, inv_d, p.eps)) : 0.f;
+            // a head that is not there counts as nothing: with eps = 0 the root of its zeros would be infinite
+            const float r = at >= 0 && h < y.H ? rsqrtf(fmaf(sum, inv_d, p.eps)) : 0.f;
             const QkVec<V> rr = qk_fill<V>(r), m = qk_fill<V>(-(dot * inv_d * r * r * r));   // m: what dx has of x
             ga = qk_mul<V>(ga, rr);
             gb = qk_mul<V>(gb, rr);
