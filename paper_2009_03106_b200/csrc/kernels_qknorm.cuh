@@ -332,8 +332,13 @@ qknorm_backward_kernel(const __grid_constant__ QkParams p) {
             gb[n] = qk_mul<V>(gb[n], rr);
             acc0[n] = qk_fma<V>(ga[n], xa[n], acc0[n]);
             acc1[n] = qk_fma<V>(gb[n], xb[n], acc1[n]);
-            if (head && c[n].there) qk_store<T, V>(out + c[n].a0, qk_fma<V>(m, xa[n], qk_mul<V>(ga[n], gain0[n])));
-            if (head && c[n].second) qk_store<T, V>(out + c[n].a1, qk_fma<V>(m, xb[n], qk_mul<V>(gb[n], gain1[n])));
+            if (now >= 0) {
+                if (head && c[n].there) qk_store<T, V>(out + c[n].a0, qk_fma<V>(m, xa[n], qk_mul<V>(ga[n], gain0[n])));
+                if (head && c[n].second) qk_store<T, V>(out + c[n].a1, qk_fma<V>(m, xb[n], qk_mul<V>(gb[n], gain1[n])));
+            } else {                                     // not what the products say: a gain may be NaN
+                if (head && c[n].there) qk_store<T, V>(out + c[n].a0, qk_fill<V>(0.f));
+                if (head && c[n].second) qk_store<T, V>(out + c[n].a1, qk_fill<V>(0.f));
+            }
         }
         out += o_inc;
     }
@@ -619,9 +624,12 @@ qknorm_backward_ring_kernel(const __grid_constant__ QkParams p) {
             gb = qk_mul<V>(gb, rr);
             acc0 = qk_fma<V>(ga, xa, acc0);
             acc1 = qk_fma<V>(gb, xb, acc1);
-            if (mine) {
+            if (mine && at >= 0) {
                 qk_store<T, V>(reinterpret_cast<T*>(out), qk_fma<V>(m, xa, qk_mul<V>(ga, qk_shared<V>(gain_a))));
                 qk_store<T, V>(reinterpret_cast<T*>(out + far), qk_fma<V>(m, xb, qk_mul<V>(gb, qk_shared<V>(gain_b))));
+            } else if (mine) {                            // not what the products say: a gain may be NaN
+                qk_store<T, V>(reinterpret_cast<T*>(out), qk_fill<V>(0.f));
+                qk_store<T, V>(reinterpret_cast<T*>(out + far), qk_fill<V>(0.f));
             }
             t += step; out += o_inc;
         }
