@@ -15,7 +15,8 @@ constexpr int kNumSMs = 148;        // B200: 2 dies x 74 SMs
 // if that one was launched with the programmatic-serialization attribute, start its CTAs as soon as every CTA of
 // this grid has made the call (or exited) and there is room for them; that kernel's threads call griddep_wait
 // before they touch anything this grid (or an earlier one) writes or reads for writing: the wait returns once
-// this grid has completed and its writes are visible.  Without the attribute both are no-ops.  A kernel that was itself
+// this grid has completed and its writes are visible to ordinary loads (not to read-only ones, __ldg or const __restrict__
+// pointers: those are for data that stays the same for as long as the kernel runs).  Without the attribute both are no-ops.  A kernel that was itself
 // launched so makes the call only behind its own wait: whoever follows may then read, without waiting, what lies two
 // launches back.
 __device__ __forceinline__ void griddep_launch_dependents() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }

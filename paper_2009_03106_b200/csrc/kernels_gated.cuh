@@ -267,7 +267,7 @@ struct GatedOut {
 };
 template <typename T> __device__ __forceinline__ void gated_end(const GatedOut& o, long m, int f, float g, float u) {
     constexpr bool EXACT = sizeof(T) == 4;
-    if (o.bias) { g += __ldg(o.bias + f); u += __ldg(o.bias + o.F + f); }
+    if (o.bias) { g += o.bias[f]; u += o.bias[o.F + f]; }
     float h = 0.f;
     gate_dispatch<EXACT>(o.act, [&](auto a) { h = gate_act<decltype(a)::value, EXACT>(g) * u; });
     gate_store(static_cast<T*>(o.h) + m * o.ldh + f, h);
@@ -721,7 +721,7 @@ gated_tc_kernel(const __grid_constant__ gt::Maps maps, const __grid_constant__ g
             const int row0 = w.m * 2 * BM_CTA + (int)rank * BM_CTA + quarter * 32;
             const int box_col = w.n * HN + box * 64, col = box_col + (group & 1) * 32;
             float bias_g = 0.f, bias_u = 0.f;                                // of column `lane`: to the others by shuffle
-            if (o.bias && col + lane < o.F && o.splits == 1) { bias_g = __ldg(o.bias + col + lane); bias_u = __ldg(o.bias + o.F + col + lane); }
+            if (o.bias && col + lane < o.F && o.splits == 1) { bias_g = o.bias[col + lane]; bias_u = o.bias[o.F + col + lane]; }
             // A wait that ran out must not leave the box's other warp at a barrier: from then on both only keep step.
             ok = __all_sync(0xFFFFFFFFu, ok && mbar_wait(&acc_full[buf], (it >> 1) & 1, abort_flag, p.status));
             tc_fence_after_sync();

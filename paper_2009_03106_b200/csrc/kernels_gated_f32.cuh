@@ -188,7 +188,7 @@ gated_tc3_kernel(const __grid_constant__ gt3::Maps maps, const __grid_constant__
             const int col0 = tn * (FWD ? HN : N) + at0, col1 = FWD ? col0 : col0 + CW;
             // A lane's share of the biases, for shuffles in the epilogue; loads there, one a column and lane, were 1.5 us a tile.
             float bias_g = 0.f, bias_u = 0.f;
-            if (FWD && o.bias && lane < CW && col0 + lane < o.F) { bias_g = __ldg(o.bias + col0 + lane); bias_u = __ldg(o.bias + o.F + col0 + lane); }
+            if (FWD && o.bias && lane < CW && col0 + lane < o.F) { bias_g = o.bias[col0 + lane]; bias_u = o.bias[o.F + col0 + lane]; }
             float x[2][CW];
 #pragma unroll
             for (int j = 0; j < CW; ++j) { x[0][j] = 0.f; x[1][j] = 0.f; }

@@ -336,7 +336,7 @@ zta_group_kernel(const __grid_constant__ zg::Maps maps, const __grid_constant__ 
                     for (int i = 0; i < NR; ++i) {
                         const int rl = lane + 32 * i;
                         // past the last row TMA filled zeros; the factor only has to be finite there
-                        fr[i] = blk0 + rl >= w.row_end ? 0.f : !clip ? 1.f : __ldg(clip + e_first + (uniform ? 0 : (rem0 + rl) / T));
+                        fr[i] = blk0 + rl >= w.row_end ? 0.f : !clip ? 1.f : clip[e_first + (uniform ? 0 : (rem0 + rl) / T)];
                     }
                 }
                 const bool bias_here = y.do_bias && z_live && (NORM ? o_tile == 0 : (kb % o_tiles) == o_tile);

@@ -400,8 +400,8 @@ relbias_grad_kernel(const __grid_constant__ RbGrad p) {
 // G[i][b][h] = (G +) the tiles' sums in order, sq[i] = the sum of its squares.  `lanes` threads (a power of two up to 32) share a sum.
 constexpr int RB_FINISH_THREADS = 512;
 __global__ void __launch_bounds__(RB_FINISH_THREADS)
-relbias_finish_kernel(const float* __restrict__ part, int H, int tiles, int n_buckets, int lanes, int accumulate,
-                      float* __restrict__ grads, float* __restrict__ sq) {
+relbias_finish_kernel(const float* part, int H, int tiles, int n_buckets, int lanes, int accumulate,
+                      float* grads, float* sq) {
     __shared__ float red[32];
     griddep_wait();
     griddep_launch_dependents();

@@ -35,8 +35,8 @@ stored_grad_kernel(const __grid_constant__ StoredParams p) {
 #pragma unroll
             for (int k = 0; k < UNR; ++k) {
                 const long e = (long)i + (long)k * step;
-                v[k] = e < p.B ? __ldg(p.G + (size_t)e * p.ld + c) : 0.f;
-                f[k] = e < p.B ? (p.clip ? __ldg(p.clip + e) : 1.f) : 0.f;
+                v[k] = e < p.B ? p.G[(size_t)e * p.ld + c] : 0.f;
+                f[k] = e < p.B ? (p.clip ? p.clip[e] : 1.f) : 0.f;
             }
 #pragma unroll
             for (int k = 0; k < UNR; ++k) acc = fmaf(f[k], v[k], acc);

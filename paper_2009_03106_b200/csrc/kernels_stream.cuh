@@ -50,8 +50,7 @@ t1_sqnorm_kernel(const T* __restrict__ A, long lda, const T* __restrict__ Z, lon
 // thousand, the kernel is pure latency.
 // ---------------------------------------------------------------------------
 __global__ void __launch_bounds__(256)
-factors_kernel(const float* __restrict__ sq_layers, int L, long ld_sq, int B, float C,
-               float* __restrict__ clip, float* __restrict__ norms, int* __restrict__ n_clipped) {
+factors_kernel(const float* sq_layers, int L, long ld_sq, int B, float C, float* clip, float* norms, int* n_clipped) {
     __shared__ float red[32];
     float cnt = 0.f;
     griddep_wait();
@@ -75,8 +74,7 @@ factors_kernel(const float* __restrict__ sq_layers, int L, long ld_sq, int B, fl
 // threshold C[l].  One CTA per layer.
 struct LayerThresholds { float C[64]; };
 __global__ void __launch_bounds__(256)
-factors_rows_kernel(const float* __restrict__ sq_layers, long ld_sq, int B, const LayerThresholds th,
-                    float* __restrict__ clip_layers, float* __restrict__ norms_layers) {
+factors_rows_kernel(const float* sq_layers, long ld_sq, int B, const LayerThresholds th, float* clip_layers, float* norms_layers) {
     const int l = blockIdx.x;
     const float C = th.C[l];
     griddep_wait();

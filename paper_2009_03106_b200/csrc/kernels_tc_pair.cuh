@@ -120,7 +120,7 @@ struct Params {
 
 __device__ __forceinline__ float row_factor(const Params& p, const float* clip, int e) {
     if (!DPCLIP_IN_RANGE(e, (p.R + p.T - 1) / p.T, p.status)) return 0.f;
-    return clip ? __ldg(clip + e) : 1.f;
+    return clip ? clip[e] : 1.f;
 }
 
 __host__ __device__ __forceinline__ long segment_of(long u, int S, int U, long lcm) { return u / S + u / U - u / lcm; }
