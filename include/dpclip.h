@@ -595,7 +595,7 @@ int dpclip_rotation_table(float* table, long n_pos, int rot_dim, double base, do
  * X, W, H, Z of one `dtype`; products are summed in fp32, H comes from the unrounded Z.  bf16 runs on the tensor cores (rows that are no
  * 16-byte multiples are laid out in the workspace first, or stay on the fp32 ALUs where that costs more).  M from 1
  * (one token: the weights are streamed once).  Outputs may not overlap inputs.  Large fp32 calls run on the tensor cores as six products of
- * three bf16 planes (fp32 accuracy; an infinity among the inputs can come out as NaN).
+ * three bf16 planes (fp32 accuracy; sums that are not finite are taken again from the numbers themselves, which is slow).
  *   workspace >= dpclip_gated_workspace_bytes(), its header set up by dpclip_workspace_init
  * Errors: INVALID_ARG, MISALIGNED, WORKSPACE. */
 typedef enum { DPCLIP_ACT_SILU = 0, DPCLIP_ACT_GELU = 1, DPCLIP_ACT_GELU_TANH = 2, DPCLIP_ACT_RELU = 3 } dpclip_activation;

@@ -457,8 +457,9 @@ int launch_gated_tc3(const tc::gt3::Maps& maps, const tc::gt3::Params& p, cudaSt
     const int rc = launch_after(tc::gated_tc3_kernel<FWD, HN>, dim3(2 * pairs), tc::gt3::THREADS, C::SMEM_BYTES, st, maps, p);
     return rc || p.out.splits == 1 ? rc : launch_gated_reduce<float, FWD>(p.out, st);
 }
-// The product of planes that lie in the workspace behind the partial products: those of a [M][KD], then those of w [2F][K].
-int gated_tensor_f32(bool fwd, int M, int K, int F, GatedOut out, uint8_t* ws, const GatedSpace& space, int* status, cudaStream_t st) {
+// The product of a [M][KD] and w [2F][K], whose planes lie in the workspace behind the partial products.
+int gated_tensor_f32(bool fwd, const float* a, long lda, const float* w, long ldw, int M, int K, int F, GatedOut out, uint8_t* ws,
+                     const GatedSpace& space, int* status, cudaStream_t st) {
     using namespace tc::gt3;
     const int KD = fwd ? K : 2 * F, cols = fwd ? F : K;
     const GatedCut cut = gated_cut(M, cols, KD, fwd, true);
@@ -473,6 +474,7 @@ int gated_tensor_f32(bool fwd, int M, int K, int F, GatedOut out, uint8_t* ws, c
     if (total > 0x3FFFFFFFL) return DPCLIP_ERR_UNSUPPORTED;
     p.total = (int)total;
     p.status = status; p.out = out; p.out.splits = cut.splits;
+    p.a = a; p.lda = lda; p.w = w; p.ldw = ldw; p.KD = KD;
     p.vec_h = is_aligned(out.h, 16) && out.ldh % 4 == 0;
     p.vec_z = out.z && is_aligned(out.z, 16) && out.ldz % 4 == 0 && F % 4 == 0;
     Maps maps;
@@ -714,7 +716,8 @@ int dpclip_gated_forward(const void* X, long ldx, const void* W, long ldw, const
         const GatedSplit c[2] = {{static_cast<const float*>(X), ldx, (__nv_bfloat16*)pa, up8(K), (long)(space.copy_a / 6), M, K, 0},
                                  {static_cast<const float*>(W), ldw, (__nv_bfloat16*)pw, up8(K), (long)(space.copy_w / 6), 2L * F, K, 0}};
         rc = gated_splits(c, 2, st);
-        return rc ? rc : gated_tensor_f32(true, M, K, F, out, ws, space, static_cast<int*>(workspace), st);
+        return rc ? rc : gated_tensor_f32(true, static_cast<const float*>(X), ldx, static_cast<const float*>(W), ldw, M, K, F, out, ws, space,
+                                          static_cast<int*>(workspace), st);
     }
     GatedSimt p;
     memset(&p, 0, sizeof(p));
@@ -775,7 +778,8 @@ int dpclip_gated_backward(const void* dH, long lddh, const void* Z, long ldz, co
         return gated_tensor(false, dz_ok ? dZ : s.copy, dz_ok ? lddz : s.ldc, w_ok ? W : pw, w_ok ? ldw : up8(K), M, K, F, out,
                             static_cast<int*>(workspace), st);
     }
-    if (planes) return gated_tensor_f32(false, M, K, F, out, ws, space, static_cast<int*>(workspace), st);
+    if (planes) return gated_tensor_f32(false, static_cast<const float*>(dZ), lddz, static_cast<const float*>(W), ldw, M, K, F, out, ws, space,
+                                        static_cast<int*>(workspace), st);
     GatedSimt p;
     memset(&p, 0, sizeof(p));
     p.a = dZ; p.lda = lddz; p.w = W; p.ldw = ldw; p.M = M; p.N = K; p.KD = 2 * F; p.out = out;
