@@ -592,8 +592,9 @@ int dpclip_rotation_table(float* table, long n_pos, int rot_dim, double base, do
  * K, d_out = 2F) the step's norms and clipped sums of both projections are those of a single dense layer.
  *   X  [M][K] row stride ldx;  W [2F][K] row stride ldw;  bias [2F] fp32 or NULL;  H [M][F] row stride ldh, OVERWRITTEN
  *   Z  [M][2F] row stride ldz, OVERWRITTEN with the pre-activations (for the backward pass), or NULL
- * X, W, H, Z of one `dtype`; products are summed in fp32, H comes from the unrounded Z.  bf16 runs on the tensor cores (rows that are no
- * 16-byte multiples are laid out in the workspace first, or stay on the fp32 ALUs where that costs more).  M from 1
+ * X, W, H, Z of one `dtype`; products are summed in fp32, H comes from the unrounded Z.  bf16 runs on the tensor cores; rows of X, W or
+ * dZ that do not start at 16-byte boundaries are laid out in the workspace first (with more than eight
+ * rows, and the workspace of every such call has the room for it; with up to eight they stay on the fp32 ALUs).  M from 1
  * (one token: the weights are streamed once).  Outputs may not overlap inputs.  Large fp32 calls run on the tensor cores as six products of
  * three bf16 planes (fp32 accuracy; sums that are not finite are taken again from the numbers themselves, which is slow).
  *   workspace >= dpclip_gated_workspace_bytes(), its header set up by dpclip_workspace_init

@@ -328,18 +328,21 @@ inline int gated_simt_splits(long M, long cols, long KD, bool fwd) {
     return clamp_int(2L * kNumSMs / tiles, 1, clamp_int(KD / 128, 1, 32));
 }
 inline bool gated_rows_ok(const void* p, long ld) { return is_aligned(p, 16) && ld % 8 == 0; }
-// copies pay from here on: 2 x 2F x K x 2 bytes of copied weights against 4 M F K flops at the fp32 ALUs' rate
-constexpr int kGatedCopyRows = 32;
+// bf16 rows that TMA cannot address are copied above this many rows.  The fp32 ALUs take as long at the least and far longer at most sizes (all
+// operands off, forward / backward: 9 x 64 -> 72 8.4 / 21 us, with copies 8.7 / 12; 9 x 2000 -> 5000 84 / 86, 35 / 35; 16384 x 512 -> 2048
+// 1760 / 2360, 75 / 180); up to eight rows have a forward kernel of their own, and their workspace would be as large as the weights.
+constexpr int kGatedCopyRows = 8;
 inline long up8(long n) { return (n + 7) / 8 * 8; }
 // fp32 on the tensor cores: from here on the ALUs' 4 M K F at 32 TFLOP/s take longer than three launches and the planes' way to memory
-inline bool gated_planes(long M, long K, long F) { return M > kGatedCopyRows && (double)M * K * F > 6e7; }
+inline bool gated_planes(long M, long K, long F) { return M > 32 && (double)M * K * F > 6e7; }
 struct GatedSpace { size_t part, copy_a, copy_w; };       // bytes: partial products; copies (fp32: planes) of an operand of M rows and of W
 GatedSpace gated_space(long M, long K, long F, dpclip_dtype dtype, bool fwd) {
     const long cols = fwd ? F : K, KD = fwd ? K : 2 * F, width = fwd ? 2 * F : K;
     const int simt = gated_simt_splits(M, cols, KD, fwd), tensor = gated_cut(M, cols, KD, fwd, dtype == DPCLIP_F32).splits;
     const int s = simt > tensor ? simt : tensor;
     GatedSpace g = {s > 1 ? round_up(sizeof(float) * (size_t)s * M * width, 256) : 0, 0, 0};
-    const size_t planes = dtype == DPCLIP_F32 ? (gated_planes(M, K, F) ? 3 : 0) : K % 8 || F % 8 ? 1 : 0;
+    // bf16: whether rows have to be copied depends on addresses and strides, which the size of a workspace does not know
+    const size_t planes = dtype == DPCLIP_F32 ? (gated_planes(M, K, F) ? 3 : 0) : M > kGatedCopyRows ? 1 : 0;
     g.copy_a = planes * round_up(2 * (size_t)M * up8(KD), 256);
     g.copy_w = planes * round_up(2 * (size_t)2 * F * up8(K), 256);
     return g;
@@ -699,7 +702,7 @@ int dpclip_gated_forward(const void* X, long ldx, const void* W, long ldw, const
     }
     if (dtype == DPCLIP_BF16 && tensor_cores_allowed()) {
         const bool as_is = gated_rows_ok(X, ldx) && gated_rows_ok(W, ldw);
-        if (as_is || (space.copy_w && M > kGatedCopyRows)) {
+        if (as_is || space.copy_w) {
             const void* a = X; const void* w = W;
             long lda = ldx, ldb = ldw;
             GatedCopy c[2];
@@ -738,7 +741,7 @@ int dpclip_gated_backward(const void* dH, long lddh, const void* Z, long ldz, co
     uint8_t* const ws = static_cast<uint8_t*>(workspace) + kHeaderBytes;
     const bool dz_ok = gated_rows_ok(dZ, lddz), w_ok = dX && gated_rows_ok(W, ldw);
     const bool planes = dX && dtype == DPCLIP_F32 && space.copy_w && tensor_cores_allowed();
-    const bool tensor = dX && dtype == DPCLIP_BF16 && tensor_cores_allowed() && ((dz_ok && w_ok) || (space.copy_w && M > kGatedCopyRows));
+    const bool tensor = dX && dtype == DPCLIP_BF16 && tensor_cores_allowed() && ((dz_ok && w_ok) || space.copy_w);
     uint8_t* const pa = ws + space.part, *const pw = pa + space.copy_a;
     // W first: the product then follows the kernel that writes dZ
     if (planes) {
