@@ -149,6 +149,17 @@ template <typename F> PyObject* guarded(F f) {
     return nullptr;
 }
 
+// The library's call, without the interpreter's lock: a launch may have to wait for room in the device's queue, and work in front of it may need
+// another thread of Python (a host function) to go on.  The arguments are worked out before.
+struct Unlocked {
+    PyThreadState* state = PyEval_SaveThread();
+    ~Unlocked() { PyEval_RestoreThread(state); }
+};
+template <typename F, typename... A> int call(F function, A... arguments) {
+    const Unlocked unlocked;
+    return function(arguments...);
+}
+
 // ------------------------------------------------------------------------------------------------ the calls
 // grads, clip, g, sigma, C, seed, stream_id, stream
 PyObject* stored_clipped_grad(PyObject*, PyObject* const* v, Py_ssize_t n) {
@@ -161,7 +172,7 @@ PyObject* stored_clipped_grad(PyObject*, PyObject* const* v, Py_ssize_t n) {
         if (grads.dim() < 1) throw BadValue("grads must have a dimension of examples");
         const int64_t B = grads.size(0), width = g.numel();
         if (grads.numel() != B * width) throw BadValue("g must have the size of one example's gradients");
-        return lib.dpclip_stored_clipped_grad(dense_f32(&grads, grads.sizes(), "grads"), width, size32(B), size32(width), dense_f32(clip, {B}, "clip"),
+        return call(lib.dpclip_stored_clipped_grad, dense_f32(&grads, grads.sizes(), "grads"), width, size32(B), size32(width), dense_f32(clip, {B}, "clip"),
                                               dense_f32(&g, g.sizes(), "g"), (float)a.number(3), (float)a.number(4), a.u64(5), a.u64(6), stream_of(v[7]));
     });
 }
@@ -179,7 +190,7 @@ PyObject* relbias_forward(PyObject*, PyObject* const* v, Py_ssize_t n) {
         writable(bias, "bias");
         const int64_t Tq = bias.size(1), Tk = bias.size(2);
         const dpclip_relbias c = {size32(buckets), a.int32(2), a.truth(3), a.truth(4)};
-        return lib.dpclip_relbias_forward(static_cast<const float*>(table.data_ptr()), buckets > 1 ? table.stride(0) : H, &c, size32(H), size32(Tq), size32(Tk),
+        return call(lib.dpclip_relbias_forward, static_cast<const float*>(table.data_ptr()), buckets > 1 ? table.stride(0) : H, &c, size32(H), size32(Tq), size32(Tk),
                                           a.integer(5), dtype_of(bias), bias.data_ptr(), Tq > 1 ? bias.stride(1) : Tk, bias.stride(0), stream_of(v[6]));
     });
 }
@@ -196,7 +207,7 @@ PyObject* relbias_sqnorms(PyObject*, PyObject* const* v, Py_ssize_t n) {
         if (grads.dim() != 3) throw BadValue("grads must be (B, n_buckets, H)");
         const int64_t B = dS.size(0), H = dS.size(1), Tq = dS.size(2), Tk = dS.size(3), buckets = grads.size(1);
         const dpclip_relbias c = {size32(buckets), a.int32(4), a.truth(5), a.truth(6)};
-        return lib.dpclip_relbias_sqnorms(dS.data_ptr(), Tq > 1 ? dS.stride(2) : Tk, dS.stride(1), dS.stride(0), size32(B), size32(H), size32(Tq), size32(Tk),
+        return call(lib.dpclip_relbias_sqnorms, dS.data_ptr(), Tq > 1 ? dS.stride(2) : Tk, dS.stride(1), dS.stride(0), size32(B), size32(H), size32(Tq), size32(Tk),
                                           a.integer(7), dense<int>(ql, at::kInt, {B}, "q_lens"), dense<int>(kl, at::kInt, {B}, "k_lens"), &c, dtype_of(dS),
                                           a.truth(10), dense_f32(&grads, {B, buckets, H}, "grads"), dense_f32(&sq, {B}, "sq_layer"), ws.data_ptr(),
                                           ws.nbytes(), stream_of(v[11]));
@@ -252,7 +263,7 @@ PyObject* qknorm_forward(PyObject*, PyObject* const* v, Py_ssize_t n) {
         parts[0] = heads_of(d, q, a.maybe(2), a.tensor(5), nullptr, q);
         if (k) parts[1] = heads_of(d, *k, a.maybe(3), a.tensor(6), nullptr, q);
         const Angles r = angles_of(d, a.maybe(4), v[7], a.maybe(9), q);
-        return lib.dpclip_qknorm_forward(parts, k ? 2 : 1, size32(q.size(0)), size32(q.size(1)), size32(q.size(3)), r.rot, a.truth(8), r.table, r.n_pos, r.pos,
+        return call(lib.dpclip_qknorm_forward, parts, k ? 2 : 1, size32(q.size(0)), size32(q.size(1)), size32(q.size(3)), r.rot, a.truth(8), r.table, r.n_pos, r.pos,
                                          a.integer(10), (float)a.number(11), dtype_of(q), stream_of(v[12]));
     });
 }
@@ -278,7 +289,7 @@ PyObject* qknorm_backward(PyObject*, PyObject* const* v, Py_ssize_t n) {
             sq[i] = dense_f32(s, {B}, "sq");
         }
         d.check(&ws);
-        return lib.dpclip_qknorm_backward(parts, k ? 2 : 1, size32(B), size32(q.size(1)), size32(D), r.rot, a.truth(15), r.table, r.n_pos, r.pos, a.integer(17),
+        return call(lib.dpclip_qknorm_backward, parts, k ? 2 : 1, size32(B), size32(q.size(1)), size32(D), r.rot, a.truth(15), r.table, r.n_pos, r.pos, a.integer(17),
                                           (float)a.number(18), dtype_of(q), grads, sq, ws.data_ptr(), ws.nbytes(), stream_of(v[19]));
     });
 }
@@ -322,7 +333,7 @@ PyObject* gated_forward(PyObject*, PyObject* const* v, Py_ssize_t n) {
         Matrix z = {nullptr, 0, 0, 0};
         if (Zt) { z = matrix_of(d, *Zt, type, x.rows, 2 * F, "Z"); writable(*Zt, "Z"); }
         d.check(bias); d.check(&ws);
-        return lib.dpclip_gated_forward(x.p, x.ld, w.p, w.ld, dense_f32(bias, {2 * F}, "bias"), size32(x.rows), size32(x.cols), size32(F), dtype_of(X),
+        return call(lib.dpclip_gated_forward, x.p, x.ld, w.p, w.ld, dense_f32(bias, {2 * F}, "bias"), size32(x.rows), size32(x.cols), size32(F), dtype_of(X),
                                         (dpclip_activation)a.int32(5), h.p, h.ld, z.p, z.ld, ws.data_ptr(), ws.nbytes(), stream_of(v[7]));
     });
 }
@@ -349,7 +360,7 @@ PyObject* gated_backward(PyObject*, PyObject* const* v, Py_ssize_t n) {
         }
         d.check(ws);
         if (ws) workspace_of(*ws);
-        return lib.dpclip_gated_backward(dh.p, dh.ld, z.p, z.ld, w.p, w.ld, size32(z.rows), size32(w.cols), size32(F), dtype_of(Zt), (dpclip_activation)a.int32(5),
+        return call(lib.dpclip_gated_backward, dh.p, dh.ld, z.p, z.ld, w.p, w.ld, size32(z.rows), size32(w.cols), size32(F), dtype_of(Zt), (dpclip_activation)a.int32(5),
                                          dz.p, dz.ld, dx.p, dx.ld, ws ? ws->data_ptr() : nullptr, ws ? ws->nbytes() : 0, stream_of(v[7]));
     });
 }
