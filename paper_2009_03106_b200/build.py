@@ -2,6 +2,7 @@
 from __future__ import annotations
 
 import glob
+import importlib.metadata
 import os
 import subprocess
 import sys
@@ -11,6 +12,7 @@ CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(os.path.dirname(HERE), "include")
 LIB = os.path.join(HERE, "libdpclip.so")
 MARSHAL = os.path.join(HERE, "_marshal.so")                # Python module: arguments of the transformer-block calls
+MARSHAL_KEY = os.path.join(HERE, "build", "marshal.key")   # what _marshal.so was built for
 LIB_DEBUG = os.path.join(HERE, "libdpclip_debug.so")       # -DDPCLIP_DEBUG: range-checked accesses
 
 NVCC_FLAGS = ["-std=c++17", "-O3", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo",
@@ -40,10 +42,25 @@ def _object_stale(obj: str, dep: str) -> bool:
     return any(not os.path.exists(n) or os.path.getmtime(n) > t for n in own)
 
 
+def _marshal_built_for() -> str:
+    """What the module is compiled against beside its sources: the C++ interfaces of torch and of the interpreter."""
+    return f"torch {importlib.metadata.version('torch')}, Python {sys.version}"
+
+
+def _marshal_stale() -> bool:
+    if not (os.path.exists(MARSHAL) and os.path.exists(MARSHAL_KEY)):
+        return True
+    with open(MARSHAL_KEY) as f:
+        if f.read() != _marshal_built_for():
+            return True
+    t = os.path.getmtime(MARSHAL)
+    return any(os.path.getmtime(d) > t for d in (os.path.join(CSRC, "marshal.cpp"), os.path.join(INCLUDE, "dpclip.h")))
+
+
 def _start_marshal(force: bool):
-    """Start compiling csrc/marshal.cpp, where it is newer than the module; None where there is nothing to do."""
-    src, dep = os.path.join(CSRC, "marshal.cpp"), os.path.join(INCLUDE, "dpclip.h")
-    if not force and os.path.exists(MARSHAL) and os.path.getmtime(MARSHAL) >= max(os.path.getmtime(src), os.path.getmtime(dep)):
+    """Start compiling csrc/marshal.cpp, where the module is older or was built for another torch or Python; None where there is nothing to do."""
+    src = os.path.join(CSRC, "marshal.cpp")
+    if not force and not _marshal_stale():
         return None
     import sysconfig
 
@@ -65,6 +82,9 @@ def _finish_marshal(started) -> None:
     if p.wait() != 0:
         raise subprocess.CalledProcessError(p.returncode, cmd)
     os.replace(tmp, MARSHAL)
+    os.makedirs(os.path.dirname(MARSHAL_KEY), exist_ok=True)
+    with open(MARSHAL_KEY, "w") as f:
+        f.write(_marshal_built_for())
 
 
 def build(force: bool = False, verbose: bool = False, debug: bool = False) -> str:
