@@ -564,7 +564,7 @@ size_t dpclip_relbias_workspace_bytes(int B, int H, int Tq, int Tk, int n_bucket
  *   positions [B * T] device or NULL: position pos0 + t.  A token whose position is negative or not below n_pos is padding: the forward
  *             pass leaves its rows of `out` as they are, the backward pass writes zeros there and counts nothing of it.
  * D <= 512, any width and alignment; widths and strides in multiples of 16 bytes are fastest.
- * Errors: INVALID_ARG, MISALIGNED, UNSUPPORTED (D > 512, B * T above 2^31 - 2^16; backward: B > 65535, T * H above 2^30). */
+ * Errors: INVALID_ARG, MISALIGNED, UNSUPPORTED (D > 512, B * T above 2^31 - 2^16, more than 65535 heads; backward: B > 65535, T * H above 2^30). */
 typedef struct {
     const void* x;  long x_example, x_token, x_head;
     const void* dy; long dy_example, dy_token, dy_head;     /* backward: signal at the output; else NULL */

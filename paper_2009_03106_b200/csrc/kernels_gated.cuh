@@ -501,7 +501,8 @@ constexpr int A_BYTES = BM_CTA * 128;                    // 128 rows x 64 bf16
 constexpr int BOX_BYTES = 32 * 128;                      // 32 rows x 64 bf16 of an output
 // Epilogue warps and the boxes of outputs they stage.  Forward: 16 warps, each 32 rows x 32 columns of h (and of zg, zu); two neighbours fill a
 // box together.  (With 8 warps of 64 columns the epilogue's latency, not its 0.24 of the issue slots, paced the kernel: 133 us.)  h is staged where
-// zg was, once that has left: a box less leaves shared memory for another stage (32768 x 512 -> 2048 with z: 137 -> 132 us).  Backward: 8 warps,
+// zg was, once that has left: a box less leaves shared memory for another stage (32768 x 512 -> 2048 with z:
+// 137 -> 132 us in short runs; call after call the power cap makes it 151 to 158).  Backward: 8 warps,
 // each 32 rows x HN columns of dx.
 template <bool FWD, bool KEEP, int HN> struct Cfg {
     static constexpr int EPI_WARPS = FWD ? 16 : 8, THREADS = 64 + 32 * EPI_WARPS;
@@ -513,8 +514,8 @@ template <bool FWD, bool KEEP, int HN> struct Cfg {
 };
 // Rows r0 .. r1 - 1 (r0 a multiple of 8) of a box to rows that TMA cannot address (bases or lengths that are no multiple of 16 bytes): a row's
 // 64 columns per warp, as 32-bit words from its first 4-byte boundary on.  The path is bound by instructions, so what depends on a row's
-// parity alone (odd lengths alternate) is worked out once for the even and once for the odd rows (20000 x 576 -> 1170 with z kept: 103 us; element
-// by element 124; the same with 1176 columns by TMA 69).  `n`: columns there are.
+// parity alone (odd lengths alternate) is worked out once for the even and once for the odd rows (20000 x 576 -> 1170 with z kept: 104 us; element
+// by element 124; the same with 1176 columns by TMA 60).  `n`: columns there are.
 __device__ __forceinline__ void box_rows_out(const uint8_t* box, __nv_bfloat16* to, long ld, int r0, int r1, int n, int lane) {
     uint32_t lo[2], hi[2];
     __nv_bfloat16* at[2];

@@ -12,7 +12,7 @@
 //
 // Bound: memory in long calls (every input is read once, every output written once), round trips in short ones.  The backward pass computes
 // rms(x) again from the x it reads anyway, so the forward pass stores nothing for it.  128 x 256 tokens in bf16: 8 + 8 heads of 64 in 30 us (134
-// MB, what a copy takes), backward 16 + 2 heads of 128 in 105 us (453 MB).
+// MB, what a copy takes), backward 16 + 2 heads of 128 in 103 us (453 MB).
 #pragma once
 #include "common.cuh"
 
@@ -372,7 +372,7 @@ qknorm_backward_kernel(const __grid_constant__ QkParams p) {
 // The same passes with the loads taken out of the way: every lane copies its own runs of the warp's next tokens into shared memory
 // (cp.async, 16 bytes, zero-filled where nothing is read), STAGES - 1 of them ahead, and reads back only what it copied itself, so a warp
 // waits for its own copies and for no other warp.  With loads to registers, four heads in flight a group, the forward pass took 38 us where it
-// takes 30, the backward pass 135 (113; 105 since its chunks fill whole waves).  A warp stays with one block of heads.
+// takes 30, the backward pass 135 (113; 103 since its chunks fill whole waves).  A warp stays with one block of heads.
 __device__ __forceinline__ void qk_copy16(uint32_t dst, const void* src, bool on) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(on ? 16 : 0) : "memory");
 }
@@ -460,9 +460,10 @@ template <int V> struct QkAngles {
     }
 };
 
-constexpr int QK_FWD_STAGES = 6, QK_BWD_STAGES = 3;      // backward: 126 us with three, 134 with four, 136 with six (453 MB)
+constexpr int QK_FWD_STAGES = 6, QK_BWD_STAGES = 3;      // backward: 126 us with three, 134 with four, 136 with six (453 MB, before its chunks filled whole waves)
 
-// A warp's walk is over the tokens of the whole batch: blockIdx.x * WARPS + warp, step gridDim.x * WARPS.
+// A warp's walk is over the tokens of the whole batch: blockIdx.x * WARPS + warp, step gridDim.x * WARPS.  Three CTAs an SM leave a thread 80
+// registers, and the bf16 forms keep 1 to 23 words of the walks in local memory.
 template <typename T, int V, int G, bool INTER>
 __global__ void __launch_bounds__(QK_THREADS, 3)
 qknorm_forward_ring_kernel(const __grid_constant__ QkParams p) {
