@@ -596,7 +596,8 @@ int dpclip_rotation_table(float* table, long n_pos, int rot_dim, double base, do
  * dZ that do not start at 16-byte boundaries are laid out in the workspace first (with more than eight
  * rows, and the workspace of every such call has the room for it; with up to eight they stay on the fp32 ALUs).  M from 1
  * (one token: the weights are streamed once).  Outputs may not overlap inputs.  Large fp32 calls run on the tensor cores as six products of
- * three bf16 planes (fp32 accuracy; sums that are not finite are taken again from the numbers themselves, which is slow).
+ * three bf16 planes (fp32 accuracy; sums that come out as NaN, as infinities make them there, are taken again from the
+ * numbers themselves, which is slow).
  *   workspace >= dpclip_gated_workspace_bytes(), its header set up by dpclip_workspace_init
  * Errors: INVALID_ARG, MISALIGNED, WORKSPACE. */
 typedef enum { DPCLIP_ACT_SILU = 0, DPCLIP_ACT_GELU = 1, DPCLIP_ACT_GELU_TANH = 2, DPCLIP_ACT_RELU = 3 } dpclip_activation;
